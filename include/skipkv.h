@@ -16,7 +16,9 @@
  * tokens (skipkv_token_redundancy) with the selection that uses it (skipkv_select_fill_red), the per-step append
  * (skipkv_append, skipkv_append_step) and its fusion with the attention (skipkv_decode_step), and the same steps
  * over a paged cache (skipkv_score_paged, skipkv_compact_paged, skipkv_decode_attn_paged,
- * skipkv_decode_step_paged).
+ * skipkv_decode_step_paged); a cache held in 8 bits with a scale for each block of tokens (skipkv_pack_q8,
+ * skipkv_append_q8, skipkv_append_step_q8, skipkv_decode_attn_q8, skipkv_unpack_q8); and the page server of a paged
+ * cache (skipkv_page_tables, skipkv_slot_map).
  *
  * Conventions
  *   - Every pointer marked "device" is a CUDA device pointer; "host" is ordinary memory.
@@ -65,6 +67,8 @@ extern "C" {
 #define SKIPKV_STATUS_COMPACT_TIMEOUT 0x1u  /* compaction hand-off wait ran out; rows of that slab are unspecified */
 #define SKIPKV_STATUS_COPY_TIMEOUT    0x2u  /* a bulk copy did not complete within the wait limit */
 #define SKIPKV_STATUS_BAD_TABLE       0x4u  /* a sentence table was inconsistent (offsets beyond cap, n_sent > max_sent) */
+#define SKIPKV_STATUS_NOT_FINITE      0x8u  /* a row to be held in 8 bits had an infinity or a NaN */
+#define SKIPKV_STATUS_NO_PAGES        0x10u /* the pool had too few free pages for all that was asked of it */
 
 typedef struct {
     int32_t batch;        /* sequences                                                        */
@@ -418,6 +422,127 @@ int skipkv_decode_step_paged(const skipkv_shape* shape, const void* q, const voi
 int skipkv_decode_attn_static(const skipkv_shape* shape, const void* q, const void* K, const void* V,
                               const int32_t* kv_len, void* out, void* hidden, const void* steer_vec,
                               const float* alpha, const uint8_t* flag, uint32_t* status, void* stream);
+
+/*
+ * The cache in 8 bits.  (The paper keeps its cache in the model's 16 bits; this halves the bytes that decode attention
+ * reads of what the eviction left.)  A row keeps its 128 channels, one byte each: a code c, which stands for the value
+ * c * s, where s is the scale that block_rows consecutive tokens of a (sequence, KV head) slab share; K and V have scales of
+ * their own.  SKIPKV_Q8_E4M3: c is a float of 4 exponent and 3 mantissa bits, |c| <= 448.  SKIPKV_Q8_INT8: c is a whole number,
+ * |c| <= 127.  Block i of a slab covers its tokens [i * block_rows, (i + 1) * block_rows).
+ *
+ * Two layouts, as in 16 bits:
+ *   contiguous slabs (block_table NULL): row of (b, h, t) as above, 128 bytes per row; the scale of block i of slab (b, h) at
+ *     k_scale[(b * Hk + h) * max_blocks + i].  A slab has room for min(cap[b], max_blocks * block_rows) tokens.
+ *   paged (block_table device int32 [batch][Hk][max_pages]): token t in row t % SKIPKV_PAGE_ROWS of page
+ *     block_table[b][h][t / SKIPKV_PAGE_ROWS], 16 KB per page and tensor; the scales lie by page, block i of page p at
+ *     k_scale[p * (SKIPKV_PAGE_ROWS / block_rows) + i].  A slab has room for min(cap[b], max_pages * SKIPKV_PAGE_ROWS) tokens.
+ * What the storing calls write: s is a power of two, the smallest that brings the largest finite magnitude of the block's rows to
+ * at most 448 (E4M3) or 127 (INT8), 2^-100 at least; c = value / s rounded to nearest even.  An infinity is stored as the largest
+ * code of its sign, a NaN as 0, and SKIPKV_STATUS_NOT_FINITE is raised.  Codes and scales are the same bits from run to run.
+ * The reading calls take any positive scales.  Rows that lie outside the buffers (a page that is not in [0, rows / SKIPKV_PAGE_ROWS),
+ * a slab that reaches beyond `rows`) are neither read nor written: SKIPKV_STATUS_BAD_TABLE is raised, and attention goes on
+ * without them.
+ */
+#define SKIPKV_Q8_E4M3 0
+#define SKIPKV_Q8_INT8 1
+
+typedef struct {
+    int32_t format;       /* SKIPKV_Q8_E4M3 or SKIPKV_Q8_INT8                                   */
+    int32_t block_rows;   /* tokens that share a scale: 16, 32, 64 or 128                       */
+    int32_t max_blocks;   /* contiguous slabs: row stride of the scale tables                   */
+    int32_t max_pages;    /* paged: row stride of the block table                               */
+    int32_t device;       /* ordinal of the device that has the buffers, which must then be the
+                             current one; -1: not checked                                       */
+    int32_t reserved;     /* 0 */
+    int64_t rows;         /* rows (of 128 bytes) in each of the K and V buffers                 */
+    void*   K;            /* device, 16-byte aligned                                            */
+    void*   V;
+    float*  k_scale;      /* device                                                             */
+    float*  v_scale;
+    const int32_t* block_table;   /* device, or NULL: contiguous slabs                          */
+} skipkv_q8_cache;
+
+/*
+ * skipkv_pack_q8 -- the live rows of bf16 slabs into an 8-bit cache, from each slab's first block on: what a program does with
+ * a layer when its eviction pass is done.  K, V: device bf16, contiguous slabs of `shape` (read only; shape->total_rows is their row
+ * count).  kv_len: device [batch][Hk].  A slab with more rows than the cache has room for is left out, and
+ * SKIPKV_STATUS_BAD_TABLE is raised.  Rows and scales behind the live ones are not written.
+ */
+int skipkv_pack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* K, const void* V,
+                   const int32_t* kv_len, void* ws, void* stream);
+
+/*
+ * skipkv_append_q8 -- new tokens behind the cached ones: the next part of the prompts, or one token of each sequence.
+ * k_new, v_new: device bf16 [n_new][Hk][128]; sequence b brings rows [new_off[b], new_off[b + 1]) (new_off: device
+ * int32 [batch + 1], ascending within [0, n_new]; NULL: row b alone, n_new = batch), which become its tokens kv_len_in[b][h],
+ * kv_len_in[b][h] + 1, ... .  kv_len_out[b][h] = kv_len_in[b][h] + rows; a different buffer (the caller swaps the two).
+ * Where the first new rows join a block that has rows, its scale becomes the larger of the one it had and the one that
+ * the new rows need; if it grows, the codes of the rows that it had are rounded again under it.  (So 128 tokens appended one by
+ * one are not quite what one call with all of them leaves: a code may have been rounded more than once.)  A slab without room for
+ * all its rows is left unchanged and raises SKIPKV_STATUS_BAD_TABLE.
+ */
+int skipkv_append_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* k_new, const void* v_new,
+                     const int32_t* new_off, int32_t n_new, const int32_t* kv_len_in, int32_t* kv_len_out, void* ws,
+                     void* stream);
+
+/*
+ * skipkv_append_step_q8 -- skipkv_append_step into an 8-bit cache: one token of each sequence is appended as by skipkv_append_q8
+ * (new_off NULL), and the range list and the observation window are updated as by skipkv_append_step.  Lengths go from kv_len_in
+ * to kv_len_out, a different buffer.
+ */
+int skipkv_append_step_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* k_new, const void* v_new,
+                          const int32_t* kv_len_in, int32_t* kv_len_out, int32_t* sent_off, int32_t* sent_id,
+                          int32_t* n_sent, const uint8_t* new_sent, const int32_t* gen_id, void* q_win, const void* q,
+                          int32_t slot, void* ws, void* stream);
+
+/*
+ * skipkv_decode_attn_q8 -- skipkv_decode_attn over an 8-bit cache: out[b][q] = sum_t softmax_t(q[b][q] . (s_k c_k)[t] / sqrt(d))
+ * (s_v c_v)[t] for t < kv_len[b][q / n]; the codes take part as they are, sums and softmax are those of 32 bits; bf16 result;
+ * kv_len == 0 gives zeros.  Lengths beyond a slab's room are taken as the room.  Everything else, the steering add included, as
+ * skipkv_decode_attn.
+ */
+int skipkv_decode_attn_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* q, const int32_t* kv_len,
+                          void* out, void* hidden, const void* steer_vec, const float* alpha, const uint8_t* flag, void* ws,
+                          void* stream);
+
+/*
+ * skipkv_unpack_q8 -- the live rows of an 8-bit cache as bf16 slabs, for the calls that read 16 bits: scoring and compaction
+ * of a layer (then skipkv_pack_q8 again).  K[row of (b, h, t)] = bf16(s_k c_k), rounded to nearest even, for t < kv_len[b][h]; V the
+ * same.  K, V: device bf16, contiguous slabs of `shape`, shape->total_rows rows; either may be NULL.  Other rows are not written.
+ */
+int skipkv_unpack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const int32_t* kv_len, void* K, void* V,
+                     void* ws, void* stream);
+
+/*
+ * skipkv_page_tables -- which pages of the pool each slab holds, brought in line with the tokens it needs room for: pages for
+ * prompts that arrive and for slabs that enter their next page, and back what an eviction or a finished sequence leaves behind.  (Beside the
+ * paper: the page server of its second host, on the GPU, so that lengths never come to the CPU.)  Per slab s = (b, h) with
+ * have = n_pages_in[s] and want = ceil(need[s] / SKIPKV_PAGE_ROWS):
+ *   want > have: entries [have, want) of its row of block_table get pages from the ring of free pages, n_pages_out[s] = want.
+ *     Slabs are served in index order; where the pages that are free run out, that slab and all later ones that want more
+ *     get none, n_pages_out[s] = have, and SKIPKV_STATUS_NO_PAGES is raised.
+ *   want < have: the pages of entries [want, have) go back to the ring, n_pages_out[s] = want (the entries are left as they were).
+ * need, n_pages_in: device int32 [batch][Hk]; n_pages_out: the same, a different buffer.  block_table: device int32
+ * [batch][Hk][max_pages].  free_ring: device int32 [pool_pages], the free pages in a circle, first come first served: ring_in (device
+ * int32 [2]) = {place of the first free page, how many there are}; ring_out: the same after the call, a different buffer.  Pages that
+ * come back in a call are handed out from the next call on.  The order is that of the slabs: the same tables from run to run.
+ * need < 0, need beyond max_pages pages, n_pages_in outside [0, max_pages]: that slab is left as it is and SKIPKV_STATUS_BAD_TABLE is
+ * raised; so it is where the ring is inconsistent (a page outside the pool, more pages than the pool has).  status: device uint32,
+ * nullable, bits are OR-ed in.  At most 8192 slabs (SKIPKV_ERR_UNSUPPORTED).
+ */
+int skipkv_page_tables(int32_t batch, int32_t n_kv_heads, int32_t max_pages, int32_t pool_pages, const int32_t* need,
+                       const int32_t* n_pages_in, int32_t* n_pages_out, int32_t* block_table, int32_t* free_ring,
+                       const int32_t* ring_in, int32_t* ring_out, uint32_t* status, void* stream);
+
+/*
+ * skipkv_slot_map -- the pool row of every new token: slots[i][h] = block_table[b][h][t / SKIPKV_PAGE_ROWS] * SKIPKV_PAGE_ROWS +
+ * t % SKIPKV_PAGE_ROWS with t = start[b][h] + i - new_off[b], for new_off[b] <= i < new_off[b + 1]; -1 where the slab holds no
+ * page for t (t / SKIPKV_PAGE_ROWS >= n_pages[b][h]).  An index for the caller's own copies into the pool.  start, n_pages: device
+ * int32 [batch][Hk].  new_off: device int32 [batch + 1], ascending, or NULL: token i belongs to sequence i.  slots: device int64
+ * [n_new][Hk]; entries of tokens that belong to no sequence are not written.  n_new = 0 does nothing.
+ */
+int skipkv_slot_map(int32_t batch, int32_t n_kv_heads, int32_t max_pages, const int32_t* block_table, const int32_t* n_pages,
+                    const int32_t* start, const int32_t* new_off, int32_t n_new, int64_t* slots, void* stream);
 
 #ifdef __cplusplus
 }

@@ -287,6 +287,125 @@ def append_token(sent_off, sent_id, new_sentence, gen_id):
     return np.asarray(new_off, np.int32), np.asarray(ids, np.int32)
 
 
+# ------------------------------------------------------------------ the cache in 8 bits
+def q8_values(fmt):
+    """O16  The value of each of the 256 codes.  "int8": two's complement.  "e4m3": sign, 4 exponent bits with bias 7, 3 mantissa bits,
+    subnormals below 2^-6, all ones (0x7f, 0xff) NaN and no infinities."""
+    c = np.arange(256)
+    if fmt == "int8":
+        return np.where(c < 128, c, c - 256).astype(np.float64)
+    e, m = (c >> 3) & 15, c & 7
+    v = np.where(e == 0, m * 2.0 ** -9, (8 + m) * 2.0 ** (e - 10.0))
+    v[(c & 127) == 127] = np.nan
+    return np.where(c < 128, v, -v)
+
+
+Q8_TOP = {"e4m3": 448.0, "int8": 127.0}
+
+
+def q8_nearest(y, fmt):
+    """O17  Codes nearest to the values y (64 bits; at most the largest code in magnitude, or infinite: the largest of that sign; NaN: 0): of
+    two equally near ones the one with an even last bit.  Found among all codes by search."""
+    y = np.nan_to_num(np.asarray(y, np.float64), nan=0.0, posinf=np.inf, neginf=-np.inf)
+    v = q8_values(fmt)
+    codes = np.array([i for i in range(256) if np.isfinite(v[i]) and abs(v[i]) <= Q8_TOP[fmt] and not (fmt == "e4m3" and i == 128)])
+    codes = codes[np.argsort(v[codes], kind="stable")]
+    grid = v[codes]
+    y = np.clip(y, grid[0], grid[-1])
+    hi = np.clip(np.searchsorted(grid, y), 1, len(grid) - 1)
+    lo = hi - 1
+    below, above = y - grid[lo], grid[hi] - y
+    pick_hi = (above < below) | ((above == below) & (codes[hi] % 2 == 0))
+    out = codes[np.where(pick_hi, hi, lo)].astype(np.uint8)
+    if fmt == "e4m3":                                                         # a value that rounds to zero keeps its sign
+        out = np.where((v[out] == 0) & np.signbit(y), 128, out).astype(np.uint8)
+    return out
+
+
+def q8_scale(x, fmt):
+    """O18  The scale of a block: the smallest power of two with max |finite x| <= top * scale, 2^-100 at least."""
+    x = np.abs(np.asarray(x, np.float64))
+    x = x[np.isfinite(x)]
+    amax = float(x.max()) if x.size else 0.0
+    e = -100
+    while amax > Q8_TOP[fmt] * 2.0 ** e:
+        e += 1
+    return 2.0 ** e
+
+
+def q8_append(codes, scale, old, x, block, fmt):
+    """O19  Rows x [n][128] behind the `old` ones of one slab, in place: codes uint8 [cap][128], scale [blocks].  The scale of a block that
+    has rows grows to what the new ones need, and its codes are rounded again under it.  Returns old + n."""
+    x = np.asarray(x, np.float64)
+    t, end = old, old + len(x)
+    while t < end:
+        i = t // block
+        stop = min((i + 1) * block, end)
+        s = q8_scale(x[t - old:stop - old], fmt)
+        if t > i * block and t == old:                                        # the block has rows
+            s = max(s, float(scale[i]))
+            if s != float(scale[i]):
+                held = slice(i * block, t)
+                codes[held] = q8_nearest(q8_values(fmt)[codes[held]] * (float(scale[i]) / s), fmt)
+        codes[t:stop] = q8_nearest(x[t - old:stop - old] / s, fmt)
+        scale[i] = s
+        t = stop
+    return end
+
+
+def q8_rows(codes, scale, n, block, fmt):
+    """O20  The first n rows of a slab in 64 bits."""
+    return q8_values(fmt)[codes[:n]] * np.asarray(scale, np.float64)[np.arange(n) // block][:, None]
+
+
+def attn_rows(q, K, V):
+    """O21  The attention equation of Section 4.1 with one query per head, over rows in 64 bits: q [n][d], K and V [N][d]."""
+    if len(K) == 0:
+        return np.zeros_like(np.asarray(q, np.float64))
+    x = np.asarray(q, np.float64) @ K.T / np.sqrt(K.shape[1])
+    p = np.exp(x - x.max(axis=1, keepdims=True))
+    return p @ V / p.sum(axis=1, keepdims=True)
+
+
+# ------------------------------------------------------------------ page server
+def page_tables(need, n_pages, table, ring, head, free, page_rows=128):
+    """O22  Pages to slabs and back, one slab after the other.  need, n_pages int [slabs]; table [slabs][max_pages] and ring [pool] are updated
+    in place; the pages that come back are put behind those that were free before the call.  Returns (n_pages, head, free, short)."""
+    pool, out = len(ring), [int(p) for p in n_pages]
+    left, at, short = free, head, False
+    back = []
+    for s in range(len(need)):
+        want = -(-int(need[s]) // page_rows)
+        if want > out[s]:
+            if short or want - out[s] > left:
+                short = True
+                continue
+            for j in range(out[s], want):
+                table[s][j] = ring[at]
+                at = (at + 1) % pool
+            left -= want - out[s]
+            out[s] = want
+        elif want < out[s]:
+            back += [int(table[s][j]) for j in range(want, out[s])]
+            out[s] = want
+    for i, p in enumerate(back):
+        ring[(head + free + i) % pool] = p
+    return np.asarray(out, np.int32), at, left + len(back), short
+
+
+def slot_map(table, n_pages, start, new_off, n_kv_heads, n_new, fill, page_rows=128):
+    """O23  Pool rows of the new tokens: table [slabs][max_pages], n_pages and start [slabs], new_off [batch + 1].  Entries of no sequence keep
+    `fill`; tokens whose page the slab does not hold get -1."""
+    out = np.full((n_new, n_kv_heads), fill, np.int64)
+    for b in range(len(new_off) - 1):
+        for i in range(int(new_off[b]), int(new_off[b + 1])):
+            for h in range(n_kv_heads):
+                s = b * n_kv_heads + h
+                t = int(start[s]) + i - int(new_off[b])
+                out[i, h] = int(table[s][t // page_rows]) * page_rows + t % page_rows if t // page_rows < n_pages[s] else -1
+    return out
+
+
 # ------------------------------------------------------------------ batch drivers
 def score_batch(shape, K_bits, qwin_bits, kv_len, sent_off, n_sent, sigma, tau, eps, want_tok_imp=False):
     """shape: dict(batch,Hq,Hk,d,alpha,max_sent,slab_off,cap).  Returns dict of arrays."""

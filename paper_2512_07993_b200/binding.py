@@ -29,7 +29,11 @@ SYMBOLS = ["skipkv_workspace_bytes", "skipkv_workspace_init", "skipkv_status", "
            "skipkv_select_fill", "skipkv_compact_fill", "skipkv_token_redundancy",
            "skipkv_append_step", "skipkv_decode_attn_paged",
            "skipkv_decode_step", "skipkv_set_wait_limit", "skipkv_wait_probe", "skipkv_select_fill_red",
-           "skipkv_score_paged", "skipkv_compact_paged", "skipkv_decode_step_paged"]
+           "skipkv_score_paged", "skipkv_compact_paged", "skipkv_decode_step_paged", "skipkv_pack_q8", "skipkv_append_q8",
+           "skipkv_append_step_q8", "skipkv_decode_attn_q8", "skipkv_unpack_q8", "skipkv_page_tables", "skipkv_slot_map"]
+PAGE_ROWS = 128                                           # SKIPKV_PAGE_ROWS
+STATUS_NOT_FINITE, STATUS_NO_PAGES = 0x8, 0x10            # SKIPKV_STATUS_*
+Q8_FORMATS = {torch.float8_e4m3fn: 0, torch.int8: 1}      # SKIPKV_Q8_*, by the type of the tensors that hold the codes
 
 
 class SkipKVError(RuntimeError):
@@ -48,6 +52,12 @@ class Shape(C.Structure):
 class Params(C.Structure):
     _fields_ = [("sigma", C.c_float), ("tau", C.c_float), ("eps", C.c_float),
                 ("budget", C.c_int32), ("protect_tail", C.c_int32)]
+
+
+class Q8Cache(C.Structure):
+    _fields_ = [("format", C.c_int32), ("block_rows", C.c_int32), ("max_blocks", C.c_int32), ("max_pages", C.c_int32),
+                ("device", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("K", C.c_void_p), ("V", C.c_void_p),
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("block_table", C.c_void_p)]
 
 
 def lib():
@@ -119,6 +129,39 @@ def make_shape(batch, n_q_heads, n_kv_heads, head_dim, window, d_model, max_sent
 
 def make_params(sigma=0.1, tau=0.95, eps=1e-6, budget=0, protect_tail=0) -> Params:
     return Params(sigma, tau, eps, budget, protect_tail)
+
+
+def make_q8_cache(K: torch.Tensor, V: torch.Tensor, k_scale: torch.Tensor, v_scale: torch.Tensor, block_rows: int,
+                  block_table: Optional[torch.Tensor] = None) -> Q8Cache:
+    """One layer's cache in 8 bits, as the ``_q8`` calls take it (it keeps the tensors alive).
+
+    K, V: codes [rows][128], ``torch.float8_e4m3fn`` or ``torch.int8`` (which says how they are read).  Scales: float32,
+    [batch][Hk][max_blocks] for contiguous slabs, [pages][128 / block_rows] with a block table (int32 [batch][Hk][max_pages])."""
+    if K.dtype not in Q8_FORMATS or V.dtype != K.dtype:
+        raise ValueError(f"codes are torch.float8_e4m3fn or torch.int8, K and V alike: got {K.dtype}, {V.dtype}")
+    if K.dim() != 2 or K.shape[1] != 128 or K.shape != V.shape:
+        raise ValueError(f"codes are [rows][128], K and V alike: got {tuple(K.shape)}, {tuple(V.shape)}")
+    if block_rows not in (16, 32, 64, 128):
+        raise ValueError(f"block_rows is 16, 32, 64 or 128: got {block_rows}")
+    if k_scale.shape != v_scale.shape:
+        raise ValueError("k_scale and v_scale of different shapes")
+    if block_table is None:
+        if k_scale.dim() != 3:
+            raise ValueError("scales of contiguous slabs are [batch][Hk][max_blocks]")
+        max_blocks, max_pages = int(k_scale.shape[2]), 0
+    else:
+        if block_table.dim() != 3 or K.shape[0] % PAGE_ROWS:
+            raise ValueError("a paged cache is whole pages of 128 rows behind a block table [batch][Hk][max_pages]")
+        if tuple(k_scale.shape) != (K.shape[0] // PAGE_ROWS, PAGE_ROWS // block_rows):
+            raise ValueError(f"scales of a paged cache are [pages][{PAGE_ROWS // block_rows}]: got {tuple(k_scale.shape)}")
+        max_blocks, max_pages = PAGE_ROWS // block_rows, int(block_table.shape[2])
+    tensors = (K, V, k_scale, v_scale) + (() if block_table is None else (block_table,))
+    if len({t.device for t in tensors}) != 1:
+        raise ValueError("the tensors of one cache are on one device")
+    c = Q8Cache(Q8_FORMATS[K.dtype], block_rows, max_blocks, max_pages, K.device.index if K.is_cuda else -1, 0, K.shape[0], _ptr(K), _ptr(V),
+                _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), _ptr(block_table, torch.int32))
+    c._keepalive = tensors
+    return c
 
 
 def skipkv_workspace_bytes(shape: Shape) -> int:
@@ -299,6 +342,54 @@ def skipkv_decode_attn_static(shape, q, K, V, kv_len, out, hidden, steer_vec, al
                                                                status, stream)
     if rc:
         _check(rc, "skipkv_decode_attn_static")
+
+
+def skipkv_pack_q8(shape, cache, K, V, kv_len, ws, stream=None) -> None:
+    rc = (_native or _load_native()).skipkv_pack_q8(shape, cache, K, V, kv_len, ws, stream)
+    if rc:
+        _check(rc, "skipkv_pack_q8")
+
+
+def skipkv_append_q8(shape, cache, k_new, v_new, new_off, n_new, kv_len_in, kv_len_out, ws, stream=None) -> None:
+    rc = (_native or _load_native()).skipkv_append_q8(shape, cache, k_new, v_new, new_off, n_new, kv_len_in, kv_len_out, ws,
+                                                      stream)
+    if rc:
+        _check(rc, "skipkv_append_q8")
+
+
+def skipkv_append_step_q8(shape, cache, k_new, v_new, kv_len_in, kv_len_out, sent_off, sent_id, n_sent, new_sent, gen_id, q_win,
+                          q, slot, ws, stream=None) -> None:
+    rc = (_native or _load_native()).skipkv_append_step_q8(shape, cache, k_new, v_new, kv_len_in, kv_len_out, sent_off, sent_id,
+                                                           n_sent, new_sent, gen_id, q_win, q, slot, ws, stream)
+    if rc:
+        _check(rc, "skipkv_append_step_q8")
+
+
+def skipkv_decode_attn_q8(shape, cache, q, kv_len, out, hidden, steer_vec, alpha, flag, ws, stream=None) -> None:
+    rc = (_native or _load_native()).skipkv_decode_attn_q8(shape, cache, q, kv_len, out, hidden, steer_vec, alpha, flag, ws, stream)
+    if rc:
+        _check(rc, "skipkv_decode_attn_q8")
+
+
+def skipkv_unpack_q8(shape, cache, kv_len, K, V, ws, stream=None) -> None:
+    rc = (_native or _load_native()).skipkv_unpack_q8(shape, cache, kv_len, K, V, ws, stream)
+    if rc:
+        _check(rc, "skipkv_unpack_q8")
+
+
+def skipkv_page_tables(batch, n_kv_heads, max_pages, pool_pages, need, n_pages_in, n_pages_out, block_table, free_ring, ring_in,
+                       ring_out, status=None, stream=None) -> None:
+    rc = (_native or _load_native()).skipkv_page_tables(batch, n_kv_heads, max_pages, pool_pages, need, n_pages_in, n_pages_out,
+                                                        block_table, free_ring, ring_in, ring_out, status, stream)
+    if rc:
+        _check(rc, "skipkv_page_tables")
+
+
+def skipkv_slot_map(batch, n_kv_heads, max_pages, block_table, n_pages, start, new_off, n_new, slots, stream=None) -> None:
+    rc = (_native or _load_native()).skipkv_slot_map(batch, n_kv_heads, max_pages, block_table, n_pages, start, new_off, n_new, slots,
+                                                     stream)
+    if rc:
+        _check(rc, "skipkv_slot_map")
 
 
 class DeviceLayer:

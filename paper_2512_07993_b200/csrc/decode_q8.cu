@@ -1,0 +1,454 @@
+// skipkv_decode_attn_q8: GQA decode attention over a cache held in 8 bits, with the steering add in the same launch.
+//
+// out = sum_t softmax_t(q . (s_k c_k)[t] / sqrt(d)) (s_v c_v)[t].  A block's scale is one number for 16 tokens or more, so it never touches the
+// codes: s_k multiplies 16 logits of a head at once, s_v the tile's share of the output sums.  Every live row is read once, 256 bytes
+// per token and slab.
+//  * Work = tiles of 128 tokens (a page) enumerated over all (sequence, head) slabs and cut into equal contiguous ranges, one per CTA, one
+//    CTA per SM; each (CTA, slab) intersection gives one partial (maximum, sum, 128 sums per head); the last CTA that delivers one for a slab
+//    merges them.
+//  * Eight warps, each with its own 16 rows of every tile and its own ring of asynchronous copies (three stages of 4 KB): no barrier in the
+//    stream.  With half the bytes per row a tile's chain of latencies must be hidden twice as well as over a bf16 cache: two warps
+//    to a scheduler.
+//  * Products in f16 on the tensor cores (mma.sync m16n8k16; a query row per head is far below a tcgen05 tile): every code of either format
+//    is an f16 value, and a query head, shifted by a power of two so that its largest magnitude is in [2^14, 2^15), is one down to 2^-38 of
+//    that.  The order of channels in S = K Q^T and of tokens and channels in O^T = V^T P^T is free, so a lane takes 16 bytes of a row as they
+//    lie: 32 consecutive channels of a key row (two 16-byte loads), 16 consecutive channels of four value rows, of which byte permutes
+//    make pairs of tokens.  Rows are 128 bytes; their 16-byte pieces lie permuted (piece c of row r at c ^ (r & 7)), so neither
+//    load has bank conflicts.
+//  * The probabilities go in as two f16 parts of 2^15 p, 22 bits of the fp32 value, absolute 2^-40 for small ones; a tile's products are added to the
+//    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates).  Up to four heads per group the
+//    eight columns hold high and low parts side by side.
+#include "common.cuh"
+#include "mma.cuh"
+#include "q8.cuh"
+#include "steer.cuh"
+
+namespace skipkv {
+
+constexpr int kQdWarps = 8;
+constexpr int kQdThreads = kQdWarps * 32;
+constexpr int kQdRows = 16;                                   // rows of a tile that one warp works on
+static_assert(kQdWarps * kQdRows == kQ8Tile, "a tile is a page");
+constexpr int kQdStages = 3;
+constexpr int kQdStageBytes = 2 * kQdRows * kQ8RowBytes;      // one warp's key rows, then its value rows
+constexpr int kQdRingBytes = kQdWarps * kQdStages * kQdStageBytes;
+constexpr int kQdMaxGrid = 256;
+static_assert(kQdStageBytes >= kMaxGroup * kHeadDim * 4, "a warp's sums of a segment fit into a stage");
+
+// D[16 x 8] += A[16 x 16] B[16 x 8], f16 operands, fp32 accumulators; the first form has no sum to add to
+__device__ __forceinline__ void mma16816h(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16816h_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+                 : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+// two probabilities as two f16 parts each
+__device__ __forceinline__ void split_f16(float2 x, uint32_t& hi, uint32_t& lo) {
+    hi = pack_f16(x.x, x.y);
+    const float2 r = __ffma2_rn(f16x2_to_f2(hi), make_float2(-1.f, -1.f), x);
+    lo = pack_f16(r.x, r.y);
+}
+__device__ __forceinline__ uint4 lds128(uint32_t addr) {
+    uint4 r;
+    asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr) : "memory");
+    return r;
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
+}
+
+// kFew: up to four heads per group (the eight columns are then the heads twice)
+template <int kFmt, bool kFew>
+__global__ void __launch_bounds__(kQdThreads, 2)
+decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, const __nv_bfloat16* q, Q8View c,
+                 const int32_t* kv_len, __nv_bfloat16* out, uint32_t* status, uint32_t* dec_cnt, float* dec_part, int d_model,
+                 __nv_bfloat16* hidden, const __nv_bfloat16* steer_vec, const float* alpha, const uint8_t* flag) {
+    extern __shared__ __align__(128) uint8_t dsm[];
+    const int n = Hq / Hk;                                                   // heads per group
+    int* pref = reinterpret_cast<int*>(dsm + kQdRingBytes);                  // [n_slabs + 1] tile prefix
+    int* lens = pref + n_slabs + 1;                                          // [n_slabs]
+    __shared__ __align__(16) float s_scale[kQdWarps][kQdStages][2];          // of the key and value rows in each stage
+    __shared__ float2 s_ml[kQdWarps][kMaxGroup];                             // a segment's maxima and sums
+    __shared__ uint32_t s_wsum[kQdWarps];
+    __shared__ int s_last;
+
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int G = gridDim.x, cta = blockIdx.x;
+    pdl_wait();
+
+    // ---- schedule: CTA k has the tiles [k T / Ge, (k + 1) T / Ge) of the T tiles, Ge = the CTAs that have work
+    for (int s = tid; s < n_slabs; s += kQdThreads) lens[s] = min(max(kv_len[s], 0), q8_room(c, cap, Hk, s));
+    __syncthreads();
+    cta_prefix<kQdThreads>(n_slabs, [&](int s) { return (lens[s] + kQ8Tile - 1) / kQ8Tile; }, pref, s_wsum);
+    const int T = pref[n_slabs], Ge = min(G, T);
+    const int t_begin = cta < Ge ? int((long long)cta * T / Ge) : T, t_end = cta < Ge ? int((long long)(cta + 1) * T / Ge) : T;
+    int slab = 0;
+    {
+        int hi = n_slabs - 1;                             // slab holding tile t_begin: the last one with pref <= t_begin
+        while (slab < hi) {
+            const int mid = (slab + hi + 1) >> 1;
+            if (pref[mid] <= t_begin) slab = mid; else hi = mid - 1;
+        }
+    }
+    pdl_trigger();
+
+    // ---- copies: this warp's 16 rows of the CTA's k-th tile, and their two scales, go to stage k % kQdStages
+    const uint32_t ring = smem_u32(dsm) + warp * kQdStages * kQdStageBytes;
+    const int c_row = lane >> 3, c_col = lane & 7;
+    int p_t = t_begin, p_slab = slab, p_stage = 0;
+    uint32_t bad = 0;                                     // stages whose rows lie outside the buffers
+    auto issue_next = [&]() {
+        if (p_t < t_end) {
+            while (pref[p_slab + 1] <= p_t) ++p_slab;
+            const int j = p_t - pref[p_slab], left = lens[p_slab] - j * kQ8Tile, rows = left - warp * kQdRows;
+            bad &= ~(1u << p_stage);
+            if (rows > 0) {
+                const Q8Tile at = q8_tile(c, slab_off, cap, Hk, p_slab, j, min(left, kQ8Tile));
+                if (at.row < 0) {
+                    bad |= 1u << p_stage;
+                    if (lane == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+                } else {
+                    const size_t off = size_t(at.row + warp * kQdRows + c_row) * kQ8RowBytes + size_t(c_col) * 16;
+                    const uint8_t *kp = c.K + off, *vp = c.V + off;
+                    const uint32_t dst = ring + p_stage * kQdStageBytes + c_row * kQ8RowBytes;
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        // row 4 i + c_row: its place is c_col ^ (row & 7)
+                        const uint32_t d = dst + i * 4 * kQ8RowBytes + ((c_col ^ c_row ^ ((i & 1) << 2)) << 4);
+                        const int bytes = c_row + 4 * i < rows ? 16 : 0;
+                        cp_async16(d, bytes ? kp + i * 4 * kQ8RowBytes : c.K, bytes);
+                        cp_async16(d + kQdRows * kQ8RowBytes, bytes ? vp + i * 4 * kQ8RowBytes : c.V, bytes);
+                    }
+                    if (lane < 2)
+                        cp_async4(smem_u32(&s_scale[warp][p_stage][lane]), (lane ? c.v_scale : c.k_scale) + at.scale + ((warp * kQdRows) >> c.block_log2));
+                }
+            }
+            ++p_t;
+            if (++p_stage == kQdStages) p_stage = 0;
+        }
+        cp_async_commit();                                // empty groups keep the count
+    };
+#pragma unroll 1
+    for (int k = 0; k < kQdStages - 1; ++k) issue_next();
+
+    {
+        const int side0 = (warp * G + cta) * 32 + lane, side_step = G * kQdThreads;
+        const int vec_per_row = d_model / 8, steer_total = hidden != nullptr ? batch * vec_per_row : 0;
+#pragma unroll 1
+        for (int i = side0; i < steer_total; i += side_step)
+            steer_store(i, vec_per_row, hidden, steer_load(i, vec_per_row, hidden, steer_vec, alpha, flag));
+    }
+
+    const int g = lane >> 2, qd = lane & 3;               // mma fragments: rows (tokens, channels) g and g + 8, columns (heads) 2 qd and 2 qd + 1
+    // Queries of a slab: column g (head) of the B operand, channels 32 qd + 4 ks + {0, 1} and {2, 3} in step ks, times 2^shift; unshift
+    // takes the two heads of the accumulator's columns back.
+    uint32_t qa[8][2];
+    float2 unshift = make_float2(1.f, 1.f);
+    auto load_q = [&](int slab_) {
+        const int hd = kFew ? g & 3 : g;                  // head of this lane's column
+        const uint4* qp = reinterpret_cast<const uint4*>(q + (size_t(slab_ / Hk) * Hq + size_t(slab_ % Hk) * n + min(hd, n - 1)) * kHeadDim + qd * 32);
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 v = hd < n ? qp[i] : make_uint4(0u, 0u, 0u, 0u);
+            qa[2 * i][0] = v.x; qa[2 * i][1] = v.y; qa[2 * i + 1][0] = v.z; qa[2 * i + 1][1] = v.w;
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) m = __vmaxu2(m, __vmaxu2(qa[i][0] & 0x7fff7fffu, qa[i][1] & 0x7fff7fffu));
+        m = max(m & 0xffffu, m >> 16);
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
+        m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
+        const int field = min(max(268 - int(m >> 7), 1), 253);     // of 2^shift: the largest magnitude goes to [2^14, 2^15)
+        const float up = __uint_as_float(uint32_t(field) << 23);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int k = 0; k < 2; ++k) {
+                const float2 v = bf16x2_to_f2(qa[i][k]);
+                qa[i][k] = pack_f16(v.x * up, v.y * up);
+            }
+        const float down = __uint_as_float(uint32_t(254 - field) << 23);
+        unshift = make_float2(__shfl_sync(0xffffffffu, down, 8 * qd), __shfl_sync(0xffffffffu, down, 8 * qd + 4));
+    };
+
+    const float qscale = 1.4426950408889634f * rsqrtf(float(kHeadDim));
+    const uint32_t k_base = ring + g * kQ8RowBytes + (((2 * qd) ^ g) << 4);             // and ^ 16; row g + 8: + 8 rows
+    const uint32_t v_row0 = ring + (kQdRows + 2 * qd) * kQ8RowBytes;
+    const uint32_t v_col0 = uint32_t(g ^ (2 * qd)) << 4, v_col1 = uint32_t(g ^ (2 * qd + 1)) << 4;
+
+    int t = t_begin, c_stage = 0;
+    while (t < t_end) {
+        // -------------------------------------------------------------- one (CTA, slab) segment
+        while (pref[slab + 1] <= t) ++slab;
+        const int seg_end = min(t_end, pref[slab + 1]);
+        const int b = slab / Hk, h = slab % Hk;
+        load_q(slab);
+        float2 acc[8][2];                                 // channels 16 g + 2 j and 16 g + 2 j + 1 of the lane's two heads
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[j][0] = acc[j][1] = make_float2(0.f, 0.f);
+        float2 m = make_float2(-INFINITY, -INFINITY), l = make_float2(0.f, 0.f);    // their running maximum, this lane's share of the sum
+        int rows_left = lens[slab] - (t - pref[slab]) * kQ8Tile - warp * kQdRows;     // of this warp's part of the tile
+        for (; t < seg_end; ++t, rows_left -= kQ8Tile) {
+            cp_async_wait<kQdStages - 2>();
+            __syncwarp();                                 // every lane's pieces have landed; the stage before is read out
+            const bool live = rows_left > 0 && !((bad >> c_stage) & 1u);
+            issue_next();
+            if (live) {
+                const uint32_t stage = c_stage * kQdStageBytes;
+                const float ks = s_scale[warp][c_stage][0], vs = s_scale[warp][c_stage][1];
+                float s[4][4];                            // four chains of two steps each
+                {
+                    const uint4 k0 = lds128(k_base + stage), k1 = lds128((k_base + stage) ^ 16u);
+                    const uint4 k2 = lds128(k_base + stage + 8 * kQ8RowBytes), k3 = lds128((k_base + stage + 8 * kQ8RowBytes) ^ 16u);
+                    const uint32_t lo[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w}, hi[8] = {k2.x, k2.y, k2.z, k2.w, k3.x, k3.y, k3.z, k3.w};
+#pragma unroll
+                    for (int i = 0; i < 8; ++i) {
+                        uint32_t a0, a1, a2, a3;
+                        q8_to_f16<kFmt>(lo[i], a0, a2);
+                        q8_to_f16<kFmt>(hi[i], a1, a3);
+                        if (i < 4) mma16816h_first(s[i], a0, a1, a2, a3, qa[i][0], qa[i][1]);
+                        else       mma16816h(s[i - 4], a0, a1, a2, a3, qa[i][0], qa[i][1]);
+                    }
+                }
+                const uint4 v0 = lds128(v_row0 + stage + v_col0), v1 = lds128(v_row0 + stage + kQ8RowBytes + v_col1);
+                const uint4 v2 = lds128(v_row0 + stage + 8 * kQ8RowBytes + v_col0), v3 = lds128(v_row0 + stage + 9 * kQ8RowBytes + v_col1);
+                // this lane's logits: tokens g and g + 8 of its two heads (packed fp32 arithmetic: a pair of heads per instruction)
+                const float f = qscale * ks;
+                const float2 f2 = make_float2(f * unshift.x, f * unshift.y);
+                auto sum = [&](int k) {
+                    return __fmul2_rn(__fadd2_rn(__fadd2_rn(make_float2(s[0][k], s[0][k + 1]), make_float2(s[1][k], s[1][k + 1])),
+                                                 __fadd2_rn(make_float2(s[2][k], s[2][k + 1]), make_float2(s[3][k], s[3][k + 1]))), f2);
+                };
+                float2 x = sum(0), y = sum(2);
+                if (rows_left < kQdRows) {
+                    if (g >= rows_left) x = make_float2(-INFINITY, -INFINITY);
+                    if (g + 8 >= rows_left) y = make_float2(-INFINITY, -INFINITY);
+                }
+                float2 top = make_float2(fmaxf(x.x, y.x), fmaxf(x.y, y.y));
+                if (__any_sync(0xffffffffu, top.x > m.x || top.y > m.y)) {
+#pragma unroll
+                    for (int d = 4; d < 32; d <<= 1) {
+                        top.x = fmaxf(top.x, __shfl_xor_sync(0xffffffffu, top.x, d));
+                        top.y = fmaxf(top.y, __shfl_xor_sync(0xffffffffu, top.y, d));
+                    }
+                    top = make_float2(fmaxf(top.x, m.x), fmaxf(top.y, m.y));
+                    const float2 sc = make_float2(ex2(m.x - top.x), ex2(m.y - top.y));   // first rows: 2^(-inf) = 0
+                    l = __fmul2_rn(l, sc);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) { acc[j][0] = __fmul2_rn(acc[j][0], sc); acc[j][1] = __fmul2_rn(acc[j][1], sc); }
+                    m = top;
+                }
+                // 2^15 p
+                const float2 neg = make_float2(15.f - m.x, 15.f - m.y);
+                x = __fadd2_rn(x, neg); y = __fadd2_rn(y, neg);
+                x = make_float2(ex2(x.x), ex2(x.y)); y = make_float2(ex2(y.x), ex2(y.y));
+                l = __fadd2_rn(l, __fadd2_rn(x, y));
+                uint32_t hx, lx, hy, ly;
+                split_f16(x, hx, lx);
+                split_f16(y, hy, ly);
+                uint32_t ph0, ph1, pl0 = 0u, pl1 = 0u;
+                if (kFew) {
+                    const bool first = qd < 2;            // this lane's columns hold high parts (the others low ones)
+                    ph0 = movmatrix_trans(first ? hx : lx); ph1 = movmatrix_trans(first ? hy : ly);
+                } else {
+                    ph0 = movmatrix_trans(hx); ph1 = movmatrix_trans(hy);
+                    pl0 = movmatrix_trans(lx); pl1 = movmatrix_trans(ly);
+                }
+                const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
+                const uint32_t w2[4] = {v2.x, v2.y, v2.z, v2.w}, w3[4] = {v3.x, v3.y, v3.z, v3.w};
+                const float2 vs2 = make_float2(vs, vs);
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {         // channels 16 g + 4 w + 2 u and the next; tokens 2 qd, 2 qd + 1 and 8 more
+                        const uint32_t pick = u ? 0x7362u : 0x5140u;
+                        uint32_t a0, a1, a2, a3;
+                        q8_to_f16<kFmt>(__byte_perm(w0[w], w1[w], pick), a0, a1);
+                        q8_to_f16<kFmt>(__byte_perm(w2[w], w3[w], pick), a2, a3);
+                        float d[4];
+                        mma16816h_first(d, a0, a1, a2, a3, ph0, ph1);
+                        if (!kFew) mma16816h(d, a0, a1, a2, a3, pl0, pl1);
+                        const int j = 2 * w + u;
+                        acc[j][0] = __ffma2_rn(make_float2(d[0], d[1]), vs2, acc[j][0]);
+                        acc[j][1] = __ffma2_rn(make_float2(d[2], d[3]), vs2, acc[j][1]);
+                    }
+                }
+            }
+            if (++c_stage == kQdStages) c_stage = 0;
+        }
+
+        // -------------------------------------------------------------- flush this (CTA, slab) segment
+#pragma unroll
+        for (int d = 4; d < 32; d <<= 1) {
+            l.x += __shfl_xor_sync(0xffffffffu, l.x, d);
+            l.y += __shfl_xor_sync(0xffffffffu, l.y, d);
+        }
+        if (kFew) {                                       // the same heads' low parts
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    acc[j][k].x += __shfl_xor_sync(0xffffffffu, acc[j][k].x, 2);
+                    acc[j][k].y += __shfl_xor_sync(0xffffffffu, acc[j][k].y, 2);
+                }
+        }
+        // The sums go to the stage of the tile that was worked on last: its rows are read out, and the next copy into it is issued behind the
+        // barriers below.
+        const int free_stage = c_stage == 0 ? kQdStages - 1 : c_stage - 1;
+        auto sums = [&](int w) { return reinterpret_cast<float*>(dsm + (size_t(w) * kQdStages + free_stage) * kQdStageBytes); };
+        __syncwarp();
+        if (!kFew || qd < 2) {
+            float* wp = sums(warp) + size_t(2 * qd) * kHeadDim + 16 * g;
+            if (2 * qd < n) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    reinterpret_cast<float4*>(wp)[j] = make_float4(acc[2 * j][0].x, acc[2 * j][1].x, acc[2 * j + 1][0].x, acc[2 * j + 1][1].x);
+                if (g == 0) s_ml[warp][2 * qd] = make_float2(m.x, l.x);
+            }
+            wp += kHeadDim;
+            if (2 * qd + 1 < n) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    reinterpret_cast<float4*>(wp)[j] = make_float4(acc[2 * j][0].y, acc[2 * j][1].y, acc[2 * j + 1][0].y, acc[2 * j + 1][1].y);
+                if (g == 0) s_ml[warp][2 * qd + 1] = make_float2(m.y, l.y);
+            }
+        }
+        __syncthreads();
+        // merge the warps; thread -> channel of every other head
+        const int fc = int(((long long)(pref[slab] + 1) * Ge - 1) / T), lc = int(((long long)pref[slab + 1] * Ge - 1) / T);
+        const int n_part = lc - fc + 1;
+        __nv_bfloat16* o = out + (size_t(b) * Hq + size_t(h) * n) * kHeadDim;
+        float* rec = dec_part + size_t(cta + slab) * n * kDecPartStride;
+        const int ch = tid & (kHeadDim - 1);
+#pragma unroll 1
+        for (int hl = tid / kHeadDim; hl < n; hl += kQdThreads / kHeadDim) {
+            float M = -1e30f, L = 0.f, A = 0.f;           // (finite: a warp without rows has -inf)
+#pragma unroll
+            for (int w = 0; w < kQdWarps; ++w) M = fmaxf(M, s_ml[w][hl].x);
+#pragma unroll
+            for (int w = 0; w < kQdWarps; ++w) {
+                const float2 ml = s_ml[w][hl];
+                const float e = ex2(ml.x - M);
+                L = fmaf(ml.y, e, L);
+                A = fmaf(sums(w)[hl * kHeadDim + ch], e, A);
+            }
+            if (n_part == 1) {
+                o[hl * kHeadDim + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : A / L);
+            } else {
+                rec[hl * kDecPartStride + ch] = A;
+                if (ch == 0) *reinterpret_cast<float2*>(rec + hl * kDecPartStride + kHeadDim) = make_float2(M, L);
+            }
+        }
+        __syncthreads();                                  // every thread's record stores are ordered before the arrival; the sums are read
+        if (n_part > 1) {
+            if (tid == 0) {
+                const uint32_t old = arrive_acq_rel(dec_cnt + slab);
+                const int last = (old == uint32_t(n_part - 1)) ? 1 : 0;
+                if (last) dec_cnt[slab] = 0u;             // self-resetting for the next launch
+                s_last = last;
+            }
+            __syncthreads();
+            if (s_last) {
+                // a warp takes a head: a lane a partial for the weights (maximum, sum) and four channels for the sums
+                const float* r0 = dec_part + size_t(fc + slab) * n * kDecPartStride;
+                constexpr int kAhead = 10;
+                const int stride = n * kDecPartStride;
+#pragma unroll 1
+                for (int hl = warp; hl < n; hl += kQdWarps) {
+                    const float* rh = r0 + hl * kDecPartStride;
+                    float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+                    float M = -1e30f, L = 0.f;
+#pragma unroll 1
+                    for (int p0 = 0; p0 < n_part; p0 += 32) {
+                        const int cnt = min(32, n_part - p0);
+                        const bool on = lane < cnt;
+                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(rh + size_t((p0 + min(lane, cnt - 1)) * stride) + kHeadDim));
+                        float4 a[kAhead];
+#pragma unroll
+                        for (int k = 0; k < kAhead; ++k)
+                            if (k < cnt) a[k] = __ldcg(reinterpret_cast<const float4*>(rh + size_t((p0 + k) * stride)) + lane);
+                        float mx = on ? ml.x : -INFINITY;
+#pragma unroll
+                        for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                        const float Mn = fmaxf(M, mx), keep = ex2(M - Mn);
+                        const float w = on ? ex2(ml.x - Mn) : 0.f;
+                        float ls = on ? ml.y * w : 0.f;
+#pragma unroll
+                        for (int d = 16; d; d >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, d);
+                        L = fmaf(L, keep, ls);
+                        M = Mn;
+                        A.x *= keep; A.y *= keep; A.z *= keep; A.w *= keep;
+#pragma unroll 1
+                        for (int k0 = 0; k0 < cnt; k0 += kAhead) {
+#pragma unroll
+                            for (int k = 0; k < kAhead; ++k)
+                                if (k0 + k < cnt) {
+                                    const float wk = __shfl_sync(0xffffffffu, w, k0 + k);
+                                    A.x = fmaf(a[k].x, wk, A.x); A.y = fmaf(a[k].y, wk, A.y);
+                                    A.z = fmaf(a[k].z, wk, A.z); A.w = fmaf(a[k].w, wk, A.w);
+                                }
+#pragma unroll
+                            for (int k = 0; k < kAhead; ++k)
+                                if (k0 + kAhead + k < cnt) a[k] = __ldcg(reinterpret_cast<const float4*>(rh + size_t((p0 + k0 + kAhead + k) * stride)) + lane);
+                        }
+                    }
+                    const float inv = L == 0.f ? 0.f : 1.f / L;
+                    const __nv_bfloat162 o0 = __floats2bfloat162_rn(A.x * inv, A.y * inv), o1 = __floats2bfloat162_rn(A.z * inv, A.w * inv);
+                    __nv_bfloat162* oi = reinterpret_cast<__nv_bfloat162*>(o + hl * kHeadDim + lane * 4);
+                    oi[0] = o0; oi[1] = o1;
+                }
+            }
+        }
+    }
+    cp_async_wait<0>();
+    // slabs with no row to attend to: zeros (owned round-robin)
+#pragma unroll 1
+    for (int s = cta; s < n_slabs; s += G) {
+        if (lens[s]) continue;
+        __nv_bfloat16* o = out + (size_t(s / Hk) * Hq + size_t(s % Hk) * n) * kHeadDim;
+#pragma unroll 1
+        for (int i = tid; i < n * kHeadDim; i += kQdThreads) o[i] = __float2bfloat16_rn(0.f);
+    }
+}
+
+}  // namespace skipkv
+
+using namespace skipkv;
+
+extern "C" int skipkv_decode_attn_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* q, const int32_t* kv_len,
+                                     void* out, void* hidden, const void* steer_vec, const float* alpha, const uint8_t* flag, void* ws,
+                                     void* stream) {
+    if (int rc = check_shape(shape)) return rc;
+    if (int rc = check_q8(cache)) return rc;
+    if (!q || !kv_len || !out) return SKIPKV_ERR_INVALID_ARG;
+    if (hidden && (!steer_vec || !alpha || !flag || shape->d_model <= 0)) return SKIPKV_ERR_INVALID_ARG;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return SKIPKV_ERR_WORKSPACE;
+    if ((reinterpret_cast<uintptr_t>(q) & 15) || (reinterpret_cast<uintptr_t>(out) & 3)) return SKIPKV_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(hidden) | reinterpret_cast<uintptr_t>(steer_vec)) & 15) return SKIPKV_ERR_INVALID_ARG;
+    const WsLayout L = make_layout(*shape);
+    if (L.slabs > kQ8MaxSlabs) {
+        set_error_text("skipkv_decode_attn_q8: batch * n_kv_heads above 8192");
+        return SKIPKV_ERR_UNSUPPORTED;
+    }
+    uint8_t* w = static_cast<uint8_t*>(ws);
+    const size_t smem = size_t(kQdRingBytes) + size_t(2 * L.slabs + 1) * 4;
+    const int grid = num_sms() < kQdMaxGrid ? num_sms() : kQdMaxGrid;
+    const auto kernel = cache->format == SKIPKV_Q8_E4M3 ? (L.group <= 4 ? decode_q8_kernel<SKIPKV_Q8_E4M3, true> : decode_q8_kernel<SKIPKV_Q8_E4M3, false>)
+                                                        : (L.group <= 4 ? decode_q8_kernel<SKIPKV_Q8_INT8, true> : decode_q8_kernel<SKIPKV_Q8_INT8, false>);
+    SKIPKV_CUDA(launch_dependent(kernel, dim3(grid), dim3(kQdThreads), smem, static_cast<cudaStream_t>(stream), int(shape->batch),
+                                 int(shape->n_q_heads), int(shape->n_kv_heads), int(L.slabs), shape->slab_off, shape->cap,
+                                 static_cast<const __nv_bfloat16*>(q), q8_view(*cache), kv_len, static_cast<__nv_bfloat16*>(out),
+                                 &reinterpret_cast<Header*>(w + L.header)->status, reinterpret_cast<uint32_t*>(w + L.dec_cnt),
+                                 reinterpret_cast<float*>(w + L.dec_part), int(shape->d_model), static_cast<__nv_bfloat16*>(hidden),
+                                 static_cast<const __nv_bfloat16*>(steer_vec), alpha, flag));
+    return SKIPKV_OK;
+}

@@ -1,0 +1,167 @@
+// The page server of a paged cache: which slab holds which pages (skipkv_page_tables) and the pool row of every new token
+// (skipkv_slot_map).
+//
+// Tables: per slab the pages it holds and the pages that its tokens need; two prefix sums over the slabs, of the pages taken and of
+// the pages given back, say from which place of the ring each slab takes and to which it gives.  Every CTA works them out for itself from
+// the call's inputs, which the call does not change (counts and the ring's state go to other buffers), so no CTA waits for another.
+// The free pages are a ring, not a stack: pages are taken at its head and given back behind its tail, and with f free pages of P at most
+// P - f come back, so what is written is never what is read.  The order is that of the slabs, whatever the CTAs' order.
+// Latency: a prologue over the slabs and one chain ring -> table per page.
+//
+// Slots: 8 bytes written per token and head, the pages' entries read through L1 (a page serves 128 tokens).
+#include "common.cuh"
+
+namespace skipkv {
+
+constexpr int kPtThreads = 256;
+constexpr int kPtWarps = kPtThreads / 32;
+constexpr int kPtMaxSlabs = 8192;
+constexpr int kPtPageRows = SKIPKV_PAGE_ROWS;
+
+__global__ void __launch_bounds__(kPtThreads)
+page_tables_kernel(int n_slabs, int max_pages, int pool, const int32_t* need, const int32_t* have_in, int32_t* have_out, int32_t* table,
+                   int32_t* ring, const int32_t* ring_in, int32_t* ring_out, uint32_t* status) {
+    extern __shared__ __align__(16) int ptsm[];
+    int* take = ptsm;                                         // [n_slabs + 1] pages taken by the slabs before
+    int* give = take + n_slabs + 1;                           // [n_slabs + 1] pages given back by them
+    int* delta = give + n_slabs + 1;                          // [n_slabs] pages wanted beyond those held
+    __shared__ uint32_t s_wsum[kPtWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
+    pdl_trigger();
+    pdl_wait();
+    uint32_t bad = 0;
+    const int head = ring_in[0], free0 = ring_in[1];
+    const bool ring_ok = head >= 0 && head < pool && free0 >= 0 && free0 <= pool;
+    for (int s = tid; s < n_slabs; s += kPtThreads) {
+        const int have = have_in[s], rows = need[s];
+        const int want = int(((long long)rows + kPtPageRows - 1) / kPtPageRows);
+        const bool ok = ring_ok && rows >= 0 && want <= max_pages && have >= 0 && have <= max_pages;
+        if (!ok) bad = SKIPKV_STATUS_BAD_TABLE;
+        delta[s] = ok ? want - have : 0;
+    }
+    __syncthreads();
+    cta_prefix<kPtThreads>(n_slabs, [&](int s) { return max(delta[s], 0); }, take, s_wsum);
+    cta_prefix<kPtThreads>(n_slabs, [&](int s) { return max(-delta[s], 0); }, give, s_wsum);
+    auto at = [&](int place) { return place >= pool ? place - pool : place; };       // of the ring; place < 2 * pool
+    // a slab's pages are shared out over `per` warps, 32 at a time
+    const int warps = gridDim.x * kPtWarps, wid = cta * kPtWarps + warp;
+    const int per = max(1, warps / n_slabs);
+    for (int w = wid; w < n_slabs * per; w += warps) {
+        const int s = w % n_slabs, part = w / n_slabs;
+        const int d = delta[s], have = have_in[s];
+        int32_t* row = table + size_t(s) * max_pages;
+        const bool served = take[s + 1] <= free0;
+        if (part == 0 && lane == 0) {
+            have_out[s] = d > 0 && !served ? have : have + d;
+            if (d > 0 && !served) bad |= SKIPKV_STATUS_NO_PAGES;
+        }
+        if (d > 0 && served) {
+            for (int j = part * 32 + lane; j < d; j += per * 32) {
+                const int page = ring[at(head + take[s] + j)];
+                const bool ok = page >= 0 && page < pool;
+                if (!ok) bad |= SKIPKV_STATUS_BAD_TABLE;
+                row[have + j] = ok ? page : -1;
+            }
+        } else if (d < 0) {
+            for (int j = part * 32 + lane; j < -d; j += per * 32) {
+                if (free0 + give[s] + j >= pool) { bad |= SKIPKV_STATUS_BAD_TABLE; continue; }       // more pages than there are
+                ring[at(head + free0 + give[s] + j)] = row[have + d + j];
+            }
+        }
+    }
+    if (cta == 0 && tid == 0) {
+        // what was taken: the requests up to the last that fitted
+        int lo = 0, hi = n_slabs;                             // the largest s with take[s] <= free0
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (take[mid] <= free0) lo = mid; else hi = mid - 1;
+        }
+        const int taken = ring_ok ? take[lo] : 0, back = ring_ok ? min(give[n_slabs], pool - free0) : 0;
+        ring_out[0] = ring_ok ? at(head + taken) : head;
+        ring_out[1] = free0 - taken + back;
+    }
+    if (bad && status) atomicOr(status, bad);
+}
+
+// kHeads: KV heads of a token that a thread does (a 16-byte store where there are two)
+template <int kHeads>
+__global__ void __launch_bounds__(kPtThreads)
+slot_map_kernel(int batch, int Hk, int max_pages, const int32_t* table, const int32_t* n_pages, const int32_t* start, const int32_t* new_off,
+                int n_new, int64_t* slots) {
+    pdl_trigger();
+    pdl_wait();
+    const int hw = Hk / kHeads;
+    const uint32_t total = uint32_t(n_new) * uint32_t(hw);    // below 2^31
+    // a CTA takes a range of tokens, so that a thread goes from one sequence to the next only now and then
+    const uint32_t per = (total + gridDim.x - 1) / gridDim.x;
+    const uint32_t e0 = min(per * blockIdx.x, total), e1 = min(e0 + per, total);
+    int b = -1, lo = 0, hi = 0;                               // the sequence of the token before, its tokens
+    for (uint32_t e = e0 + threadIdx.x; e < e1; e += kPtThreads) {
+        const int i = int(e / uint32_t(hw)), h = int(e % uint32_t(hw)) * kHeads;
+        if (new_off == nullptr) {
+            b = i; lo = i; hi = i + 1;
+        } else if (b < 0 || i >= hi) {
+            int l = max(b, 0), r = batch;                     // the first sequence that ends behind token i
+            while (l < r) {
+                const int mid = (l + r) >> 1;
+                if (new_off[mid + 1] > i) r = mid; else l = mid + 1;
+            }
+            b = l;
+            if (b < batch) { lo = new_off[b]; hi = new_off[b + 1]; } else { lo = hi = 0x7fffffff; }
+        }
+        if (b >= batch || i < lo) continue;                   // a token of no sequence
+        int64_t v[kHeads];
+#pragma unroll
+        for (int k = 0; k < kHeads; ++k) {
+            const int s = b * Hk + h + k;
+            const long long t = (long long)start[s] + (i - lo);
+            v[k] = -1;
+            if (t >= 0 && t / kPtPageRows < min(n_pages[s], max_pages))
+                v[k] = (long long)table[size_t(s) * max_pages + size_t(t / kPtPageRows)] * kPtPageRows + t % kPtPageRows;
+        }
+        int64_t* p = slots + (long long)i * Hk + h;
+        if (kHeads == 2) *reinterpret_cast<longlong2*>(p) = make_longlong2(v[0], v[kHeads - 1]);
+        else *p = v[0];
+    }
+}
+
+}  // namespace skipkv
+
+using namespace skipkv;
+
+extern "C" int skipkv_page_tables(int32_t batch, int32_t n_kv_heads, int32_t max_pages, int32_t pool_pages, const int32_t* need,
+                                  const int32_t* n_pages_in, int32_t* n_pages_out, int32_t* block_table, int32_t* free_ring,
+                                  const int32_t* ring_in, int32_t* ring_out, uint32_t* status, void* stream) {
+    if (batch <= 0 || n_kv_heads <= 0 || max_pages <= 0 || pool_pages <= 0) return SKIPKV_ERR_INVALID_ARG;
+    if (!need || !n_pages_in || !n_pages_out || !block_table || !free_ring || !ring_in || !ring_out) return SKIPKV_ERR_INVALID_ARG;
+    if (n_pages_in == n_pages_out || need == n_pages_out || ring_in == ring_out) return SKIPKV_ERR_INVALID_ARG;
+    const int64_t slabs = int64_t(batch) * n_kv_heads;
+    if (slabs > kPtMaxSlabs) {
+        set_error_text("skipkv_page_tables: batch * n_kv_heads above 8192");
+        return SKIPKV_ERR_UNSUPPORTED;
+    }
+    // rows of the pool, places of the ring and sums over the slabs in 32 bits
+    if (int64_t(pool_pages) * SKIPKV_PAGE_ROWS > 0x7fffffff || slabs * max_pages > 0x7fffffff) return SKIPKV_ERR_UNSUPPORTED;
+    const size_t smem = size_t(3 * slabs + 2) * 4;
+    const int64_t want = (slabs * 4 + kPtWarps - 1) / kPtWarps;
+    const int grid = int(want < num_sms() ? want : num_sms());
+    SKIPKV_CUDA(launch_dependent(page_tables_kernel, dim3(grid), dim3(kPtThreads), smem, static_cast<cudaStream_t>(stream), int(slabs),
+                                 int(max_pages), int(pool_pages), need, n_pages_in, n_pages_out, block_table, free_ring, ring_in, ring_out, status));
+    return SKIPKV_OK;
+}
+
+extern "C" int skipkv_slot_map(int32_t batch, int32_t n_kv_heads, int32_t max_pages, const int32_t* block_table, const int32_t* n_pages,
+                               const int32_t* start, const int32_t* new_off, int32_t n_new, int64_t* slots, void* stream) {
+    if (batch <= 0 || n_kv_heads <= 0 || max_pages <= 0 || n_new < 0) return SKIPKV_ERR_INVALID_ARG;
+    if (!block_table || !n_pages || !start || (!slots && n_new > 0)) return SKIPKV_ERR_INVALID_ARG;
+    if (!new_off && n_new > batch) return SKIPKV_ERR_INVALID_ARG;
+    if (int64_t(batch) * n_kv_heads > 0x7fffffff || int64_t(n_new) * n_kv_heads > 0x7fffffff) return SKIPKV_ERR_UNSUPPORTED;
+    if (n_new == 0) return SKIPKV_OK;
+    const bool two = n_kv_heads % 2 == 0 && (reinterpret_cast<uintptr_t>(slots) & 15) == 0;
+    const int64_t work = int64_t(n_new) * n_kv_heads / (two ? 2 : 1);
+    const int64_t want = (work + kPtThreads - 1) / kPtThreads, most = int64_t(num_sms()) * 8;
+    const int grid = int(want < most ? want : most);
+    SKIPKV_CUDA(launch_dependent(two ? slot_map_kernel<2> : slot_map_kernel<1>, dim3(grid), dim3(kPtThreads), 0, static_cast<cudaStream_t>(stream),
+                                 int(batch), int(n_kv_heads), int(max_pages), block_table, n_pages, start, new_off, int(n_new), slots));
+    return SKIPKV_OK;
+}

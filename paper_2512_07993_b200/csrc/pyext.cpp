@@ -4,8 +4,8 @@
 // layers.  Marshalling 25 tensor arguments through ctypes (four attribute reads and one pointer object each) took 14.7 us
 // per skipkv_decode_step call and bounded that loop; here a call is one vectorcall that unpacks the tensors in place.
 // Every function is generated from the prototype in skipkv.h: the parameter's C type decides what is accepted
-//   const skipkv_shape* / const skipkv_params*   the ctypes structures of binding.py (read through the buffer protocol)
-//   int32_t*, float*, uint8_t*, uint32_t*        contiguous device tensor of that type (uint32_t: int32), or None
+//   const skipkv_shape* / skipkv_params* / skipkv_q8_cache*   the ctypes structures of binding.py (through the buffer protocol)
+//   int32_t*, int64_t*, float*, uint8_t*, uint32_t*           contiguous device tensor of that type (uint32_t: int32), or None
 //   void*                                        contiguous bfloat16 device tensor, or None
 //   int32_t, float                               numbers
 // and the trailing void* parameters are the workspace (any type) and the stream (None: the current stream).
@@ -48,6 +48,7 @@ bool tensor_ptr(PyObject* o, at::ScalarType want, void** out) {
 
 template <typename T> struct ScalarOf { static constexpr at::ScalarType value = at::ScalarType::BFloat16; };   // void*
 template <> struct ScalarOf<int32_t> { static constexpr at::ScalarType value = at::ScalarType::Int; };
+template <> struct ScalarOf<int64_t> { static constexpr at::ScalarType value = at::ScalarType::Long; };
 template <> struct ScalarOf<uint32_t> { static constexpr at::ScalarType value = at::ScalarType::Int; };
 template <> struct ScalarOf<float> { static constexpr at::ScalarType value = at::ScalarType::Float; };
 template <> struct ScalarOf<uint8_t> { static constexpr at::ScalarType value = at::ScalarType::Byte; };
@@ -64,7 +65,7 @@ bool struct_ptr(PyObject* o, const S** out) {
 
 template <typename T, bool kRaw>
 bool convert(PyObject* o, T& out) {
-    if constexpr (std::is_same_v<T, const skipkv_shape*> || std::is_same_v<T, const skipkv_params*>) {
+    if constexpr (std::is_same_v<T, const skipkv_shape*> || std::is_same_v<T, const skipkv_params*> || std::is_same_v<T, const skipkv_q8_cache*>) {
         return struct_ptr(o, &out);
     } else if constexpr (std::is_pointer_v<T>) {
         using E = std::remove_const_t<std::remove_pointer_t<T>>;
@@ -138,7 +139,9 @@ PyMethodDef methods[] = {
     ENTRY(skipkv_select_fill_red), ENTRY(skipkv_compact), ENTRY(skipkv_compact_fill), ENTRY(skipkv_compact_paged),
     ENTRY(skipkv_token_redundancy), ENTRY(skipkv_decode_attn), ENTRY(skipkv_decode_attn_paged), ENTRY(skipkv_decode_step),
     ENTRY(skipkv_decode_step_paged), ENTRY(skipkv_append), ENTRY(skipkv_append_step), ENTRY(skipkv_decode_attn_static, false),
-    ENTRY(skipkv_table_step, false), ENTRY(skipkv_steer, false),
+    ENTRY(skipkv_table_step, false), ENTRY(skipkv_steer, false), ENTRY(skipkv_pack_q8), ENTRY(skipkv_append_q8),
+    ENTRY(skipkv_append_step_q8), ENTRY(skipkv_decode_attn_q8), ENTRY(skipkv_unpack_q8), ENTRY(skipkv_page_tables, false),
+    ENTRY(skipkv_slot_map, false),
     {nullptr, nullptr, 0, nullptr}};
 #undef ENTRY
 

@@ -1,0 +1,417 @@
+// Storing bf16 rows in 8 bits (skipkv_pack_q8, skipkv_append_q8, skipkv_append_step_q8) and getting them back (skipkv_unpack_q8).
+//
+// A block of block_rows tokens of a (sequence, head) slab shares the scale s = 2^e, e the least with amax <= top * 2^e (top 448 or
+// 127): with a = f * 2^x, 1 <= f < 2, that is e = x - 8 for f <= 1.75 and x - 7 above (e4m3: 448 = 1.75 * 2^8), x - 6 for
+// f <= 127/64 and x - 5 above (int8).  Both follow from the bits of the largest bf16 magnitude alone; x / s is exact in fp32, so a code is
+// rounded once.  Powers of two, although int8 gives away half a bit of its range on average: codes that are rounded again under a
+// larger scale (a block that grows, a cache that is packed again after a compaction) then stay what one rounding gives but for ties
+// and what falls below the new spacing, and e4m3 loses nothing by them.
+//
+// The calls are bound by DRAM: 256 bytes read and 128 written per row and tensor (the other way round for loading).  Work = tiles of 128
+// tokens of one slab and tensor, aligned to 128 tokens of the slab, so a block is never shared by two CTAs; all slabs' tiles are
+// enumerated from the lengths on the GPU (ragged lengths cost nothing), K and V in turn.  A warp takes 16 rows, 16 lanes to a row (16 bytes of bf16,
+// 8 bytes of codes each), all its loads in flight together; maxima meet in shared memory where a block has more than 16 rows.
+#include "common.cuh"
+#include "q8.cuh"
+
+namespace skipkv {
+
+constexpr int kQsThreads = 256;
+constexpr int kQsWarps = kQsThreads / 32;
+static_assert(kQsWarps * 16 == kQ8Tile, "a warp takes 16 rows of a tile");
+
+// Where the rows come from, and what else a decode step writes.
+struct StoreArgs {
+    const uint4* k_src;          // pack: slabs of bf16 rows; append: [n_new][Hk][16]
+    const uint4* v_src;
+    long long src_rows;          // pack: rows of the bf16 buffers
+    const int32_t* new_off;      // append: [batch + 1], or nullptr: one row per sequence
+    int n_new;
+    const int32_t* len_in;       // pack: rows to store; append: rows already there
+    int32_t* len_out;            // append
+    // the decode step (n_sent == nullptr: none of it)
+    int32_t* sent_off;
+    int32_t* sent_id;
+    int32_t* n_sent;
+    const uint8_t* new_sent;
+    const int32_t* gen_id;
+    uint4* q_win;
+    const uint4* q;
+    int Hq, window, slot, max_sent;
+};
+
+// Exponent of the scale that the magnitude with these (finite) bf16 bits needs.
+template <int kFmt>
+__device__ __forceinline__ int scale_exp(uint32_t bits) {
+    const int x = int(bits >> 7) - 127, f = int(bits & 127u);
+    const int e = kFmt == SKIPKV_Q8_E4M3 ? x - 8 + (f > 96) : x - 6 + (f > 126);
+    return max(e, kQ8LeastExp);
+}
+
+template <int kFmt, bool kAppend>
+__global__ void __launch_bounds__(kQsThreads, 4)
+q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, Q8View c, StoreArgs a, uint32_t* status) {
+    extern __shared__ __align__(16) uint8_t qsm[];
+    int* pref = reinterpret_cast<int*>(qsm);                  // [n_slabs + 1] tile prefix
+    int2* span = reinterpret_cast<int2*>(qsm + ((size_t(n_slabs) + 2) / 2) * 8);     // [n_slabs] rows already there, rows afterwards
+    __shared__ uint32_t s_wsum[kQsWarps];
+    __shared__ uint32_t s_amax[2][kQsWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int G = gridDim.x, cta = blockIdx.x;
+    pdl_trigger();
+    pdl_wait();
+
+    // ---- which tiles there are
+    for (int s = tid; s < n_slabs; s += kQsThreads) {
+        const int room = q8_room(c, cap, Hk, s);
+        int old = 0, now = 0;
+        bool bad = false;
+        if (kAppend) {
+            const int b = s / Hk;
+            const int lo = a.new_off ? a.new_off[b] : b, hi = a.new_off ? a.new_off[b + 1] : b + 1;
+            old = a.len_in[s];
+            bad = old < 0 || lo < 0 || hi < lo || hi > a.n_new || (long long)old + (hi - lo) > room;
+            now = bad ? old : old + (hi - lo);
+        } else {
+            now = a.len_in[s];
+            bad = now < 0 || now > room || now > cap[s / Hk];
+            if (bad) now = 0;
+        }
+        if (bad && cta == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+        span[s] = make_int2(old, now);
+    }
+    __syncthreads();
+    auto tiles_of = [&](int s) { return span[s].y > span[s].x ? (span[s].y - 1) / kQ8Tile - span[s].x / kQ8Tile + 1 : 0; };
+    cta_prefix<kQsThreads>(n_slabs, tiles_of, pref, s_wsum);
+    const int T2 = 2 * pref[n_slabs];                         // K and V of a tile one after the other
+
+    const int c16 = lane & 15, half = lane >> 4;
+    const int group = 1 << (c.block_log2 - 4);                // warps to a block
+    int flip = 0;
+    for (int t2 = cta; t2 < T2; t2 += G) {
+        const int t = t2 >> 1;
+        int lo = 0, hi = n_slabs - 1;                         // slab of tile t: the last one with pref <= t
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (pref[mid] <= t) lo = mid; else hi = mid - 1;
+        }
+        const int s = lo, old = span[s].x, now = span[s].y;
+        const int j = old / kQ8Tile + (t - pref[s]);
+        const int t0 = j * kQ8Tile;                           // the tile's first token
+        const Q8Tile at = q8_tile(c, slab_off, cap, Hk, s, j, min(now - t0, kQ8Tile));
+        const uint4* src = (t2 & 1) ? a.v_src : a.k_src;
+        uint8_t* dst = ((t2 & 1) ? c.V : c.K) + at.row * kQ8RowBytes;
+        float* scale = ((t2 & 1) ? c.v_scale : c.k_scale) + at.scale;
+        bool ok = at.row >= 0;
+        // row of token tok in units of 16 bytes: src0 + tok * step
+        long long src0, step;
+        if (kAppend) {
+            const int b = s / Hk;
+            src0 = ((long long)(a.new_off ? a.new_off[b] : b) - old) * Hk + s % Hk;
+            step = Hk;
+        } else {
+            src0 = (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk);
+            step = 1;
+            ok = ok && src0 >= 0 && src0 + now <= a.src_rows;
+        }
+        if (!ok) {                                            // (uniform over the CTA)
+            if (tid == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+            continue;
+        }
+
+        // ---- the new rows among this warp's 16, and their largest magnitude
+        const int r0 = warp * 16 + half;
+        uint4 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int tok = t0 + r0 + 2 * i;
+            x[i] = make_uint4(0u, 0u, 0u, 0u);
+            if (tok >= old && tok < now) x[i] = __ldcs(src + (src0 + (long long)tok * step) * 16 + c16);
+        }
+        const int blk = (warp * 16) >> c.block_log2;          // this warp's block in the tile
+        const int b0 = t0 + (blk << c.block_log2);
+        const bool held = b0 < old;                           // the block has rows under a scale of its own
+        const float s_old = held ? scale[blk] : 0.f;
+        uint32_t m = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            m = __vmaxu2(m, __vmaxu2(x[i].x & 0x7fff7fffu, x[i].y & 0x7fff7fffu));
+            m = __vmaxu2(m, __vmaxu2(x[i].z & 0x7fff7fffu, x[i].w & 0x7fff7fffu));
+        }
+        m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
+        const bool wild = m >= 0x7f80u;
+        if (wild) {                                           // infinities and NaN do not count for the scale; a NaN becomes zero
+            if (lane == 0) atomicOr(status, SKIPKV_STATUS_NOT_FINITE);
+            uint32_t fin = 0;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    uint32_t h[2] = {w[k] & 0xffffu, w[k] >> 16};
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        if ((h[u] & 0x7fffu) > 0x7f80u) h[u] = 0u;
+                        if ((h[u] & 0x7fffu) < 0x7f80u) fin = max(fin, h[u] & 0x7fffu);
+                    }
+                    w[k] = h[0] | (h[1] << 16);
+                }
+                x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+            }
+            m = __reduce_max_sync(0xffffffffu, fin);
+        }
+        if (group > 1) {                                      // (two sets of places in turn: one barrier per tile)
+            if (lane == 0) s_amax[flip][warp] = m;
+            __syncthreads();
+            for (int w = warp & ~(group - 1), k = 0; k < group; ++k) m = max(m, s_amax[flip][w + k]);
+            flip ^= 1;
+        }
+        if (b0 >= now || b0 + (1 << c.block_log2) <= old) continue;      // no new row in the block (no barrier below)
+        int e = scale_exp<kFmt>(m);
+        float s_new = pow2f(e);
+        if (held) {                                           // a scale only grows; one that is no power of two goes to the next
+            const uint32_t bits = __float_as_uint(fminf(fmaxf(s_old, pow2f(kQ8LeastExp)), pow2f(122)));
+            const int eo = int(bits >> 23) - 127 + ((bits & 0x7fffffu) != 0u);
+            e = max(e, eo);
+            s_new = pow2f(e);
+        }
+        if (lane == 0 && (warp & (group - 1)) == 0) scale[blk] = s_new;
+        const float inv = pow2f(-e);
+
+        // ---- codes
+        const float again = held ? s_old * inv : 1.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int r = r0 + 2 * i, tok = t0 + r;
+            if (tok >= now) continue;
+            uint2* p = reinterpret_cast<uint2*>(dst + size_t(r) * kQ8RowBytes) + c16;
+            if (tok >= old) {
+                const float2 y0 = bf16x2_to_f2(x[i].x), y1 = bf16x2_to_f2(x[i].y), y2 = bf16x2_to_f2(x[i].z), y3 = bf16x2_to_f2(x[i].w);
+                float y[8] = {y0.x * inv, y0.y * inv, y1.x * inv, y1.y * inv, y2.x * inv, y2.y * inv, y3.x * inv, y3.y * inv};
+                if (kFmt == SKIPKV_Q8_INT8 && wild) {         // (an infinity: the largest code of its sign; e4m3 saturates by itself)
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) y[k] = fminf(fmaxf(y[k], -127.f), 127.f);
+                }
+                *p = make_uint2(q8_round<kFmt>(y[0], y[1], y[2], y[3]), q8_round<kFmt>(y[4], y[5], y[6], y[7]));
+            } else if (held && s_new != s_old) {              // a row of the block as it was
+                const uint2 cd = *p;
+                uint32_t f[4];
+                q8_to_f16<kFmt>(cd.x, f[0], f[1]);
+                q8_to_f16<kFmt>(cd.y, f[2], f[3]);
+                float2 y[4];
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    y[k] = f16x2_to_f2(f[k]);
+                    y[k].x *= again; y[k].y *= again;
+                }
+                *p = make_uint2(q8_round<kFmt>(y[0].x, y[0].y, y[1].x, y[1].y), q8_round<kFmt>(y[2].x, y[2].y, y[3].x, y[3].y));
+            }
+        }
+    }
+
+    if constexpr (kAppend) {
+        // ---- lengths, and the rest of a decode step: a warp to a slab
+        for (int s = cta * kQsWarps + warp; s < n_slabs; s += G * kQsWarps) {
+            const int old = span[s].x, now = span[s].y;
+            if (lane == 0) a.len_out[s] = now;
+            if (a.n_sent == nullptr) continue;
+            const int b = s / Hk, S0 = a.n_sent[s];
+            const bool ok = S0 >= 0 && S0 <= a.max_sent, opens = S0 == 0 || a.new_sent[b];
+            int32_t* so = a.sent_off + size_t(s) * (a.max_sent + 1);
+            const int S = ok && opens && S0 < a.max_sent ? S0 + 1 : S0;     // (a full list: the token joins the last sentence)
+            __syncwarp();
+            if (lane == 0 && (!ok || (now != old && opens && S == S0))) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+            if (!ok || now == old) continue;                      // (no room: reported above, tables as they were)
+            if (lane == 0 && S != S0) {
+                if (S0 == 0) so[0] = 0;
+                a.sent_id[size_t(s) * a.max_sent + S0] = a.gen_id[b];
+                a.n_sent[s] = S;
+            }
+            for (int i = S + lane; i <= a.max_sent; i += 32) so[i] = now;
+        }
+        if (a.q_win != nullptr) {
+            const int total = batch * a.Hq * 16;
+            for (int i = cta * kQsThreads + tid; i < total; i += G * kQsThreads)
+                a.q_win[(size_t(i >> 4) * a.window + a.slot) * 16 + (i & 15)] = a.q[i];
+        }
+    }
+}
+
+// Codes back to bf16: K and V of a tile in turn (one of them where the other has no destination).
+template <int kFmt>
+__global__ void __launch_bounds__(kQsThreads, 6)
+q8_load_kernel(int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, Q8View c, const int32_t* kv_len, uint4* K, uint4* V,
+               long long dst_rows, uint32_t* status) {
+    extern __shared__ __align__(16) uint8_t qsm[];
+    int* pref = reinterpret_cast<int*>(qsm);
+    int* lens = pref + n_slabs + 1;
+    __shared__ uint32_t s_wsum[kQsWarps];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const int G = gridDim.x, cta = blockIdx.x;
+    pdl_trigger();
+    pdl_wait();
+    for (int s = tid; s < n_slabs; s += kQsThreads) {
+        const int n = kv_len[s], room = min(q8_room(c, cap, Hk, s), cap[s / Hk]);
+        const bool bad = n < 0 || n > room;
+        if (bad && cta == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+        lens[s] = min(max(n, 0), max(room, 0));
+    }
+    __syncthreads();
+    cta_prefix<kQsThreads>(n_slabs, [&](int s) { return (lens[s] + kQ8Tile - 1) / kQ8Tile; }, pref, s_wsum);
+    const int per = (K ? 1 : 0) + (V ? 1 : 0), T = pref[n_slabs] * per;
+    const int c16 = lane & 15, r0 = warp * 16 + (lane >> 4);
+    for (int t2 = cta; t2 < T; t2 += G) {
+        const int t = per == 2 ? t2 >> 1 : t2;
+        const bool is_v = per == 2 ? (t2 & 1) != 0 : V != nullptr;
+        int lo = 0, hi = n_slabs - 1;
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (pref[mid] <= t) lo = mid; else hi = mid - 1;
+        }
+        const int s = lo, j = t - pref[s], rows = min(lens[s] - j * kQ8Tile, kQ8Tile);
+        const Q8Tile at = q8_tile(c, slab_off, cap, Hk, s, j, rows);
+        const long long to = (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk) + (long long)j * kQ8Tile;
+        if (at.row < 0 || to < 0 || to + rows > dst_rows) {
+            if (tid == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+            continue;
+        }
+        const uint2* src = reinterpret_cast<const uint2*>((is_v ? c.V : c.K) + at.row * kQ8RowBytes) + c16;
+        uint4* dst = (is_v ? V : K) + to * 16 + c16;
+        uint2 x[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            x[i] = make_uint2(0u, 0u);
+            if (r0 + 2 * i < rows) x[i] = __ldcs(src + (r0 + 2 * i) * 16);
+        }
+        if (warp * 16 >= rows) continue;
+        const float sc = ((is_v ? c.v_scale : c.k_scale) + at.scale)[(warp * 16) >> c.block_log2];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            uint32_t f[4], o[4];
+            q8_to_f16<kFmt>(x[i].x, f[0], f[1]);
+            q8_to_f16<kFmt>(x[i].y, f[2], f[3]);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+                const float2 y = f16x2_to_f2(f[k]);
+                const __nv_bfloat162 r = __floats2bfloat162_rn(y.x * sc, y.y * sc);
+                o[k] = *reinterpret_cast<const uint32_t*>(&r);
+            }
+            if (r0 + 2 * i < rows) dst[(r0 + 2 * i) * 16] = make_uint4(o[0], o[1], o[2], o[3]);
+        }
+    }
+}
+
+int check_q8(const skipkv_q8_cache* c) {
+    if (!c || !c->K || !c->V || !c->k_scale || !c->v_scale || c->rows <= 0) return SKIPKV_ERR_INVALID_ARG;
+    if (c->format != SKIPKV_Q8_E4M3 && c->format != SKIPKV_Q8_INT8) return SKIPKV_ERR_UNSUPPORTED;
+    if (c->block_rows != 16 && c->block_rows != 32 && c->block_rows != 64 && c->block_rows != 128) return SKIPKV_ERR_UNSUPPORTED;
+    if ((reinterpret_cast<uintptr_t>(c->K) | reinterpret_cast<uintptr_t>(c->V)) & 15) return SKIPKV_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 3) return SKIPKV_ERR_INVALID_ARG;
+    if (c->block_table ? c->max_pages <= 0 || c->rows % kQ8Tile != 0 : c->max_blocks <= 0) return SKIPKV_ERR_INVALID_ARG;
+    if (c->rows > int64_t(0x7fffffff) - 256) return SKIPKV_ERR_UNSUPPORTED;
+    if (c->device >= 0) {
+        int dev = 0;
+        SKIPKV_CUDA(cudaGetDevice(&dev));
+        if (dev != c->device) {
+            set_error_text("the 8-bit cache is on another device than the current one");
+            return SKIPKV_ERR_INVALID_ARG;
+        }
+    }
+    return SKIPKV_OK;
+}
+
+}  // namespace skipkv
+
+using namespace skipkv;
+
+static int too_many_slabs() {
+    set_error_text("8-bit cache: batch * n_kv_heads above 8192");
+    return SKIPKV_ERR_UNSUPPORTED;
+}
+
+// CTAs of a launch over at most `tiles` tiles: four (six) to an SM.
+static int store_grid(long long tiles, int per_sm) {
+    const long long most = (long long)num_sms() * per_sm;
+    return int(tiles < 1 ? 1 : tiles < most ? tiles : most);
+}
+
+template <bool kAppend>
+static int store(const skipkv_shape* shape, const skipkv_q8_cache* cache, const StoreArgs& a, long long tiles, void* ws, void* stream) {
+    const int slabs = shape->batch * shape->n_kv_heads;
+    if (slabs > kQ8MaxSlabs) return too_many_slabs();
+    const size_t smem = (size_t(slabs) + 2) / 2 * 8 + size_t(slabs) * 8;
+    SKIPKV_CUDA(launch_dependent(cache->format == SKIPKV_Q8_E4M3 ? q8_store_kernel<SKIPKV_Q8_E4M3, kAppend> : q8_store_kernel<SKIPKV_Q8_INT8, kAppend>,
+                                 dim3(store_grid(2 * tiles, 4)), dim3(kQsThreads), smem, static_cast<cudaStream_t>(stream), int(shape->batch),
+                                 int(shape->n_kv_heads), slabs, shape->slab_off, shape->cap, q8_view(*cache), a, &static_cast<Header*>(ws)->status));
+    return SKIPKV_OK;
+}
+
+static int append(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* k_new, const void* v_new, const int32_t* new_off,
+                  int32_t n_new, const int32_t* kv_len_in, int32_t* kv_len_out, StoreArgs a, void* ws, void* stream) {
+    if (n_new < 0 || (n_new > 0 && (!k_new || !v_new)) || !kv_len_in || !kv_len_out || kv_len_in == kv_len_out) return SKIPKV_ERR_INVALID_ARG;
+    if (!new_off && n_new != shape->batch) return SKIPKV_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(k_new) | reinterpret_cast<uintptr_t>(v_new)) & 15) return SKIPKV_ERR_INVALID_ARG;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return SKIPKV_ERR_WORKSPACE;
+    a.k_src = static_cast<const uint4*>(k_new); a.v_src = static_cast<const uint4*>(v_new);
+    a.new_off = new_off; a.n_new = n_new; a.len_in = kv_len_in; a.len_out = kv_len_out;
+    // a slab's new rows lie in one tile more than they fill, at most
+    const long long slabs = (long long)shape->batch * shape->n_kv_heads;
+    const long long tiles = new_off ? (long long)n_new * shape->n_kv_heads / kQ8Tile + 2 * slabs : slabs;
+    return store<true>(shape, cache, a, tiles, ws, stream);
+}
+
+extern "C" int skipkv_pack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* K, const void* V,
+                              const int32_t* kv_len, void* ws, void* stream) {
+    if (int rc = check_shape(shape)) return rc;
+    if (int rc = check_q8(cache)) return rc;
+    if (!K || !V || !kv_len) return SKIPKV_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15) return SKIPKV_ERR_INVALID_ARG;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return SKIPKV_ERR_WORKSPACE;
+    StoreArgs a{};
+    a.k_src = static_cast<const uint4*>(K); a.v_src = static_cast<const uint4*>(V);
+    a.src_rows = shape->total_rows; a.len_in = kv_len;
+    const long long tiles = (long long)shape->batch * shape->n_kv_heads * ((shape->max_cap + kQ8Tile - 1) / kQ8Tile);
+    return store<false>(shape, cache, a, tiles, ws, stream);
+}
+
+extern "C" int skipkv_append_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* k_new, const void* v_new,
+                                const int32_t* new_off, int32_t n_new, const int32_t* kv_len_in, int32_t* kv_len_out, void* ws,
+                                void* stream) {
+    if (int rc = check_shape(shape)) return rc;
+    if (int rc = check_q8(cache)) return rc;
+    return append(shape, cache, k_new, v_new, new_off, n_new, kv_len_in, kv_len_out, StoreArgs{}, ws, stream);
+}
+
+extern "C" int skipkv_append_step_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* k_new, const void* v_new,
+                                     const int32_t* kv_len_in, int32_t* kv_len_out, int32_t* sent_off, int32_t* sent_id,
+                                     int32_t* n_sent, const uint8_t* new_sent, const int32_t* gen_id, void* q_win, const void* q,
+                                     int32_t slot, void* ws, void* stream) {
+    if (int rc = check_shape(shape)) return rc;
+    if (int rc = check_q8(cache)) return rc;
+    if (!sent_off || !sent_id || !n_sent || !new_sent || !gen_id || shape->max_sent <= 0) return SKIPKV_ERR_INVALID_ARG;
+    if ((q_win != nullptr) != (q != nullptr)) return SKIPKV_ERR_INVALID_ARG;
+    if (q_win && (slot < 0 || slot >= shape->window)) return SKIPKV_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(q_win) | reinterpret_cast<uintptr_t>(q)) & 15) return SKIPKV_ERR_INVALID_ARG;
+    StoreArgs a{};
+    a.sent_off = sent_off; a.sent_id = sent_id; a.n_sent = n_sent; a.new_sent = new_sent; a.gen_id = gen_id;
+    a.q_win = static_cast<uint4*>(q_win); a.q = static_cast<const uint4*>(q);
+    a.Hq = shape->n_q_heads; a.window = shape->window; a.slot = slot; a.max_sent = shape->max_sent;
+    return append(shape, cache, k_new, v_new, nullptr, shape->batch, kv_len_in, kv_len_out, a, ws, stream);
+}
+
+extern "C" int skipkv_unpack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const int32_t* kv_len, void* K, void* V,
+                                void* ws, void* stream) {
+    if (int rc = check_shape(shape)) return rc;
+    if (int rc = check_q8(cache)) return rc;
+    if (!kv_len || (!K && !V)) return SKIPKV_ERR_INVALID_ARG;
+    if ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15) return SKIPKV_ERR_INVALID_ARG;
+    if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return SKIPKV_ERR_WORKSPACE;
+    const int slabs = shape->batch * shape->n_kv_heads;
+    if (slabs > kQ8MaxSlabs) return too_many_slabs();
+    const long long tiles = (long long)slabs * ((shape->max_cap + kQ8Tile - 1) / kQ8Tile) * ((K ? 1 : 0) + (V ? 1 : 0));
+    SKIPKV_CUDA(launch_dependent(cache->format == SKIPKV_Q8_E4M3 ? q8_load_kernel<SKIPKV_Q8_E4M3> : q8_load_kernel<SKIPKV_Q8_INT8>,
+                                 dim3(store_grid(tiles, 6)), dim3(kQsThreads), size_t(2 * slabs + 1) * 4, static_cast<cudaStream_t>(stream),
+                                 int(shape->n_kv_heads), slabs, shape->slab_off, shape->cap, q8_view(*cache), kv_len, static_cast<uint4*>(K),
+                                 static_cast<uint4*>(V), static_cast<long long>(shape->total_rows), &static_cast<Header*>(ws)->status));
+    return SKIPKV_OK;
+}
