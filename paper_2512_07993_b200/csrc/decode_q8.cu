@@ -22,6 +22,7 @@
 #include "mma.cuh"
 #include "q8.cuh"
 #include "steer.cuh"
+#include "tc.cuh"
 
 namespace skipkv {
 
@@ -32,7 +33,7 @@ static_assert(kQdWarps * kQdRows == kQ8Tile, "a tile is a page");
 constexpr int kQdStages = 3;
 constexpr int kQdStageBytes = 2 * kQdRows * kQ8RowBytes;      // one warp's key rows, then its value rows
 constexpr int kQdRingBytes = kQdWarps * kQdStages * kQdStageBytes;
-constexpr int kQdMaxGrid = 256;
+constexpr int kQdMaxGrid = 512;
 static_assert(kQdStageBytes >= kMaxGroup * kHeadDim * 4, "a warp's sums of a segment fit into a stage");
 
 // D[16 x 8] += A[16 x 16] B[16 x 8], f16 operands, fp32 accumulators; the first form has no sum to add to
@@ -69,20 +70,28 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
 // kFew: up to four heads per group (the eight columns are then the heads twice)
 template <int kFmt, bool kFew>
 __global__ void __launch_bounds__(kQdThreads, 2)
-decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, const __nv_bfloat16* q, Q8View c,
-                 const int32_t* kv_len, __nv_bfloat16* out, uint32_t* status, uint32_t* dec_cnt, float* dec_part, int d_model,
+decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, const __nv_bfloat16* q, Q8View c,
+                 const int32_t* kv_len, __nv_bfloat16* out, Header* hdr, uint32_t* dec_cnt, float* dec_part, int d_model,
                  __nv_bfloat16* hidden, const __nv_bfloat16* steer_vec, const float* alpha, const uint8_t* flag) {
-    extern __shared__ __align__(128) uint8_t dsm[];
+    extern __shared__ uint8_t dsm_raw[];
+    uint8_t* const dsm = dsm_raw + ((1024u - (smem_u32(dsm_raw) & 1023u)) & 1023u);      // (the swizzle goes by the address)
     const int n = Hq / Hk;                                                   // heads per group
     int* pref = reinterpret_cast<int*>(dsm + kQdRingBytes);                  // [n_slabs + 1] tile prefix
     int* lens = pref + n_slabs + 1;                                          // [n_slabs]
     __shared__ __align__(16) float s_scale[kQdWarps][kQdStages][2];          // of the key and value rows in each stage
     __shared__ float2 s_ml[kQdWarps][kMaxGroup];                             // a segment's maxima and sums
     __shared__ uint32_t s_wsum[kQdWarps];
-    __shared__ int s_last;
+    __shared__ __align__(8) uint64_t s_full[kQdWarps][kQdStages];            // a stage's copies have landed
+    __shared__ int s_last, s_abort;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = gridDim.x, cta = blockIdx.x;
+    if (lane == 0) {
+#pragma unroll
+        for (int i = 0; i < kQdStages; ++i) mbar_init(&s_full[warp][i], 1);
+        mbar_fence_init();
+        if (warp == 0) s_abort = 0;
+    }
     pdl_wait();
 
     // ---- schedule: CTA k has the tiles [k T / Ge, (k + 1) T / Ge) of the T tiles, Ge = the CTAs that have work
@@ -101,42 +110,67 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     }
     pdl_trigger();
 
-    // ---- copies: this warp's 16 rows of the CTA's k-th tile, and their two scales, go to stage k % kQdStages
-    const uint32_t ring = smem_u32(dsm) + warp * kQdStages * kQdStageBytes;
-    const int c_row = lane >> 3, c_col = lane & 7;
-    int p_t = t_begin, p_slab = slab, p_stage = 0;
-    uint32_t bad = 0;                                     // stages whose rows lie outside the buffers
+    // ---- copies: this warp's 16 rows of the CTA's k-th tile, and their two scales, go to stage k % kQdStages.  The cursor walks the slab
+    // parts of the tile range; divisions and the slab's tables are read once per part, a page's entry a tile ahead.
+    uint8_t* const ring_p = dsm + warp * kQdStages * kQdStageBytes;
+    const uint32_t ring = smem_u32(ring_p), limit = load_wait_limit(hdr);
+    const float* const sp = (lane & 1) ? c.v_scale : c.k_scale;
+    const uint32_t sp_dst = smem_u32(&s_scale[warp][0][lane & 1]);
+    const int per_tile = kQ8Tile >> c.block_log2, sub = (warp * kQdRows) >> c.block_log2;
+    int p_t = t_begin, p_slab = slab, p_end = t_begin, p_rows = 0, p_stage = 0;
+    int p_row = 0, p_scale = 0, p_page = 0;               // row of this warp's part, place of its scale; paged: the page
+    const int32_t* p_table = c.table;
+    uint32_t skip = 0;                                    // stages without copies: no rows, or rows that lie outside the buffers
     auto issue_next = [&]() {
         if (p_t < t_end) {
-            while (pref[p_slab + 1] <= p_t) ++p_slab;
-            const int j = p_t - pref[p_slab], left = lens[p_slab] - j * kQ8Tile, rows = left - warp * kQdRows;
-            bad &= ~(1u << p_stage);
-            if (rows > 0) {
-                const Q8Tile at = q8_tile(c, slab_off, cap, Hk, p_slab, j, min(left, kQ8Tile));
-                if (at.row < 0) {
-                    bad |= 1u << p_stage;
-                    if (lane == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+            if (p_t == p_end) {
+                while (pref[p_slab + 1] <= p_t) ++p_slab;
+                p_end = pref[p_slab + 1];
+                const int j = p_t - pref[p_slab];
+                p_rows = lens[p_slab] - j * kQ8Tile - warp * kQdRows;
+                if (c.table) {
+                    p_table = c.table + size_t(p_slab) * c.max_pages + j;
+                    p_page = *p_table;
                 } else {
-                    const size_t off = size_t(at.row + warp * kQdRows + c_row) * kQ8RowBytes + size_t(c_col) * 16;
-                    const uint8_t *kp = c.K + off, *vp = c.V + off;
-                    const uint32_t dst = ring + p_stage * kQdStageBytes + c_row * kQ8RowBytes;
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        // row 4 i + c_row: its place is c_col ^ (row & 7)
-                        const uint32_t d = dst + i * 4 * kQ8RowBytes + ((c_col ^ c_row ^ ((i & 1) << 2)) << 4);
-                        const int bytes = c_row + 4 * i < rows ? 16 : 0;
-                        cp_async16(d, bytes ? kp + i * 4 * kQ8RowBytes : c.K, bytes);
-                        cp_async16(d + kQdRows * kQ8RowBytes, bytes ? vp + i * 4 * kQ8RowBytes : c.V, bytes);
-                    }
-                    if (lane < 2)
-                        cp_async4(smem_u32(&s_scale[warp][p_stage][lane]), (lane ? c.v_scale : c.k_scale) + at.scale + ((warp * kQdRows) >> c.block_log2));
+                    const long long row0 = (long long)slab_row0(slab_off, cap, Hk, p_slab / Hk, p_slab % Hk);
+                    p_row = int(row0 < 0 ? c.rows : min(row0 + (long long)j * kQ8Tile + warp * kQdRows, c.rows));
+                    p_scale = p_slab * c.max_blocks + j * per_tile + sub;
                 }
             }
+            if (c.table) {                                // (a page outside the pool: a row at which nothing lies)
+                const bool in = uint32_t(p_page) < uint32_t(c.rows / kQ8Tile);
+                p_row = in ? p_page * kQ8Tile + warp * kQdRows : int(c.rows);
+                p_scale = in ? p_page * per_tile + sub : 0;
+                if (p_t + 1 < p_end) p_page = *++p_table;
+            }
+            const bool in = p_row + min(p_rows, kQdRows) <= int(c.rows);
+            skip &= ~(1u << p_stage);
+            if (p_rows > 0 && in) {
+                // 16 rows, also where the slab has fewer left: what follows them is not used
+                if (lane == 0) {
+                    uint64_t* const bar = &s_full[warp][p_stage];
+                    uint8_t* const to = ring_p + p_stage * kQdStageBytes;
+                    mbar_expect_tx(bar, kQdStageBytes);
+                    tma_load_2d(to, &k_map, 0, p_row, bar);
+                    tma_load_2d(to + kQdRows * kQ8RowBytes, &v_map, 0, p_row, bar);
+                }
+                if (lane < 2) cp_async4(sp_dst + p_stage * 8, sp + p_scale);
+            } else {
+                skip |= 1u << p_stage;
+                if (lane == 0) {
+                    mbar_arrive(&s_full[warp][p_stage]);
+                    if (p_rows > 0) atomicOr(&hdr->status, SKIPKV_STATUS_BAD_TABLE);
+                }
+            }
+            p_rows -= kQ8Tile;
+            p_row = min(p_row + kQ8Tile, int(c.rows));
+            p_scale += per_tile;
             ++p_t;
             if (++p_stage == kQdStages) p_stage = 0;
         }
-        cp_async_commit();                                // empty groups keep the count
+        cp_async_commit();                                // (of the scales; empty groups keep the count)
     };
+    __syncwarp();
 #pragma unroll 1
     for (int k = 0; k < kQdStages - 1; ++k) issue_next();
 
@@ -181,11 +215,13 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     };
 
     const float qscale = 1.4426950408889634f * rsqrtf(float(kHeadDim));
-    const uint32_t k_base = ring + g * kQ8RowBytes + (((2 * qd) ^ g) << 4);             // and ^ 16; row g + 8: + 8 rows
-    const uint32_t v_row0 = ring + (kQdRows + 2 * qd) * kQ8RowBytes;
-    const uint32_t v_col0 = uint32_t(g ^ (2 * qd)) << 4, v_col1 = uint32_t(g ^ (2 * qd + 1)) << 4;
+    // this lane's 16-byte pieces in a stage: pieces 2 qd and 2 qd + 1 (^ 16) of key rows g and g + 8; piece g of value rows 2 qd, 2 qd + 1 and 8 more
+    const uint32_t k_at = ring + g * kQ8RowBytes + (((2 * qd) ^ g) << 4);
+    const uint32_t v_at = ring + (kQdRows + 2 * qd) * kQ8RowBytes + ((g ^ (2 * qd)) << 4);
+    const uint32_t v_at1 = (v_at ^ 16u) + kQ8RowBytes;
 
-    int t = t_begin, c_stage = 0;
+    int t = t_begin, c_stage = 0, issued = -1;            // issued: tiles whose copies were started when a wait gave up
+    uint32_t parity = 0;
     while (t < t_end) {
         // -------------------------------------------------------------- one (CTA, slab) segment
         while (pref[slab + 1] <= t) ++slab;
@@ -197,41 +233,44 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
         for (int j = 0; j < 8; ++j) acc[j][0] = acc[j][1] = make_float2(0.f, 0.f);
         float2 m = make_float2(-INFINITY, -INFINITY), l = make_float2(0.f, 0.f);    // their running maximum, this lane's share of the sum
         int rows_left = lens[slab] - (t - pref[slab]) * kQ8Tile - warp * kQdRows;     // of this warp's part of the tile
+#pragma unroll 1
         for (; t < seg_end; ++t, rows_left -= kQ8Tile) {
             cp_async_wait<kQdStages - 2>();
-            __syncwarp();                                 // every lane's pieces have landed; the stage before is read out
-            const bool live = rows_left > 0 && !((bad >> c_stage) & 1u);
-            issue_next();
+            const bool landed = warp_wait(&s_full[warp][c_stage], parity, limit, &s_abort, &hdr->status);
+            if (!landed && issued < 0) issued = p_t - t_begin;       // from here on this warp copies nothing and works on nothing
+            const bool live = issued < 0 && !((skip >> c_stage) & 1u);
+            if (issued < 0) issue_next();
             if (live) {
-                const uint32_t stage = c_stage * kQdStageBytes;
+                const uint32_t so = c_stage * kQdStageBytes;
                 const float ks = s_scale[warp][c_stage][0], vs = s_scale[warp][c_stage][1];
-                float s[4][4];                            // four chains of two steps each
-                {
-                    const uint4 k0 = lds128(k_base + stage), k1 = lds128((k_base + stage) ^ 16u);
-                    const uint4 k2 = lds128(k_base + stage + 8 * kQ8RowBytes), k3 = lds128((k_base + stage + 8 * kQ8RowBytes) ^ 16u);
-                    const uint32_t lo[8] = {k0.x, k0.y, k0.z, k0.w, k1.x, k1.y, k1.z, k1.w}, hi[8] = {k2.x, k2.y, k2.z, k2.w, k3.x, k3.y, k3.z, k3.w};
+                float s[2][4];                            // two chains of four steps each
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) {
+                for (int half = 0; half < 2; ++half) {
+                    const uint4 k0 = lds128((k_at + so) ^ (half << 4)), k1 = lds128(((k_at + so) ^ (half << 4)) + 8 * kQ8RowBytes);
+                    const uint32_t lo[4] = {k0.x, k0.y, k0.z, k0.w}, hi[4] = {k1.x, k1.y, k1.z, k1.w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
                         uint32_t a0, a1, a2, a3;
                         q8_to_f16<kFmt>(lo[i], a0, a2);
                         q8_to_f16<kFmt>(hi[i], a1, a3);
-                        if (i < 4) mma16816h_first(s[i], a0, a1, a2, a3, qa[i][0], qa[i][1]);
-                        else       mma16816h(s[i - 4], a0, a1, a2, a3, qa[i][0], qa[i][1]);
+                        if (half == 0 && i < 2) mma16816h_first(s[i & 1], a0, a1, a2, a3, qa[4 * half + i][0], qa[4 * half + i][1]);
+                        else                    mma16816h(s[i & 1], a0, a1, a2, a3, qa[4 * half + i][0], qa[4 * half + i][1]);
                     }
                 }
-                const uint4 v0 = lds128(v_row0 + stage + v_col0), v1 = lds128(v_row0 + stage + kQ8RowBytes + v_col1);
-                const uint4 v2 = lds128(v_row0 + stage + 8 * kQ8RowBytes + v_col0), v3 = lds128(v_row0 + stage + 9 * kQ8RowBytes + v_col1);
+                uint4 v0 = lds128(v_at + so), v1 = lds128(v_at1 + so);
+                uint4 v2 = lds128(v_at + so + 8 * kQ8RowBytes), v3 = lds128(v_at1 + so + 8 * kQ8RowBytes);
                 // this lane's logits: tokens g and g + 8 of its two heads (packed fp32 arithmetic: a pair of heads per instruction)
                 const float f = qscale * ks;
                 const float2 f2 = make_float2(f * unshift.x, f * unshift.y);
-                auto sum = [&](int k) {
-                    return __fmul2_rn(__fadd2_rn(__fadd2_rn(make_float2(s[0][k], s[0][k + 1]), make_float2(s[1][k], s[1][k + 1])),
-                                                 __fadd2_rn(make_float2(s[2][k], s[2][k + 1]), make_float2(s[3][k], s[3][k + 1]))), f2);
-                };
-                float2 x = sum(0), y = sum(2);
-                if (rows_left < kQdRows) {
+                float2 x = __fmul2_rn(__fadd2_rn(make_float2(s[0][0], s[0][1]), make_float2(s[1][0], s[1][1])), f2);
+                float2 y = __fmul2_rn(__fadd2_rn(make_float2(s[0][2], s[0][3]), make_float2(s[1][2], s[1][3])), f2);
+                if (rows_left < kQdRows) {                // the end of the slab: rows behind it hold anything, NaN too
                     if (g >= rows_left) x = make_float2(-INFINITY, -INFINITY);
                     if (g + 8 >= rows_left) y = make_float2(-INFINITY, -INFINITY);
+                    if (2 * qd >= rows_left) v0 = make_uint4(0u, 0u, 0u, 0u);
+                    if (2 * qd + 1 >= rows_left) v1 = make_uint4(0u, 0u, 0u, 0u);
+                    if (2 * qd + 8 >= rows_left) v2 = make_uint4(0u, 0u, 0u, 0u);
+                    if (2 * qd + 9 >= rows_left) v3 = make_uint4(0u, 0u, 0u, 0u);
                 }
                 float2 top = make_float2(fmaxf(x.x, y.x), fmaxf(x.y, y.y));
                 if (__any_sync(0xffffffffu, top.x > m.x || top.y > m.y)) {
@@ -283,7 +322,8 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                     }
                 }
             }
-            if (++c_stage == kQdStages) c_stage = 0;
+            __syncwarp();                                 // the stage is read out: the next copies may go there
+            if (++c_stage == kQdStages) { c_stage = 0; parity ^= 1u; }
         }
 
         // -------------------------------------------------------------- flush this (CTA, slab) segment
@@ -305,7 +345,6 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
         // barriers below.
         const int free_stage = c_stage == 0 ? kQdStages - 1 : c_stage - 1;
         auto sums = [&](int w) { return reinterpret_cast<float*>(dsm + (size_t(w) * kQdStages + free_stage) * kQdStageBytes); };
-        __syncwarp();
         if (!kFew || qd < 2) {
             float* wp = sums(warp) + size_t(2 * qd) * kHeadDim + 16 * g;
             if (2 * qd < n) {
@@ -322,6 +361,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                 if (g == 0) s_ml[warp][2 * qd + 1] = make_float2(m.y, l.y);
             }
         }
+        fence_proxy_async_smem();                         // (the stage's next writer is a bulk copy)
         __syncthreads();
         // merge the warps; thread -> channel of every other head
         const int fc = int(((long long)(pref[slab] + 1) * Ge - 1) / T), lc = int(((long long)pref[slab + 1] * Ge - 1) / T);
@@ -360,7 +400,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             if (s_last) {
                 // a warp takes a head: a lane a partial for the weights (maximum, sum) and four channels for the sums
                 const float* r0 = dec_part + size_t(fc + slab) * n * kDecPartStride;
-                constexpr int kAhead = 10;
+                constexpr int kAhead = 6;
                 const int stride = n * kDecPartStride;
 #pragma unroll 1
                 for (int hl = warp; hl < n; hl += kQdWarps) {
@@ -410,6 +450,10 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
         }
     }
     cp_async_wait<0>();
+    // (every copy has been waited for; where a wait gave up, those in flight are waited for here)
+#pragma unroll 1
+    for (int k = max(issued - kQdStages, 0); k < issued; ++k)
+        (void)mbar_wait(&s_full[warp][k % kQdStages], uint32_t(k / kQdStages) & 1u, kRetirePolls);
     // slabs with no row to attend to: zeros (owned round-robin)
 #pragma unroll 1
     for (int s = cta; s < n_slabs; s += G) {
@@ -439,15 +483,19 @@ extern "C" int skipkv_decode_attn_q8(const skipkv_shape* shape, const skipkv_q8_
         set_error_text("skipkv_decode_attn_q8: batch * n_kv_heads above 8192");
         return SKIPKV_ERR_UNSUPPORTED;
     }
+    if (!cache->block_table && int64_t(L.slabs) * cache->max_blocks > 0x7fffffff) return SKIPKV_ERR_UNSUPPORTED;      // places of scales in 32 bits
     uint8_t* w = static_cast<uint8_t*>(ws);
-    const size_t smem = size_t(kQdRingBytes) + size_t(2 * L.slabs + 1) * 4;
-    const int grid = num_sms() < kQdMaxGrid ? num_sms() : kQdMaxGrid;
+    const size_t smem = 1024 + size_t(kQdRingBytes) + size_t(2 * L.slabs + 1) * 4;
+    CUtensorMap km, vm;
+    if (int rc = tmap_codes(&km, cache->K, uint64_t(cache->rows), kQdRows)) return rc;
+    if (int rc = tmap_codes(&vm, cache->V, uint64_t(cache->rows), kQdRows)) return rc;
+    const int grid = 2 * num_sms() < kQdMaxGrid ? 2 * num_sms() : kQdMaxGrid;
     const auto kernel = cache->format == SKIPKV_Q8_E4M3 ? (L.group <= 4 ? decode_q8_kernel<SKIPKV_Q8_E4M3, true> : decode_q8_kernel<SKIPKV_Q8_E4M3, false>)
                                                         : (L.group <= 4 ? decode_q8_kernel<SKIPKV_Q8_INT8, true> : decode_q8_kernel<SKIPKV_Q8_INT8, false>);
-    SKIPKV_CUDA(launch_dependent(kernel, dim3(grid), dim3(kQdThreads), smem, static_cast<cudaStream_t>(stream), int(shape->batch),
+    SKIPKV_CUDA(launch_dependent(kernel, dim3(grid), dim3(kQdThreads), smem, static_cast<cudaStream_t>(stream), km, vm, int(shape->batch),
                                  int(shape->n_q_heads), int(shape->n_kv_heads), int(L.slabs), shape->slab_off, shape->cap,
                                  static_cast<const __nv_bfloat16*>(q), q8_view(*cache), kv_len, static_cast<__nv_bfloat16*>(out),
-                                 &reinterpret_cast<Header*>(w + L.header)->status, reinterpret_cast<uint32_t*>(w + L.dec_cnt),
+                                 reinterpret_cast<Header*>(w + L.header), reinterpret_cast<uint32_t*>(w + L.dec_cnt),
                                  reinterpret_cast<float*>(w + L.dec_part), int(shape->d_model), static_cast<__nv_bfloat16*>(hidden),
                                  static_cast<const __nv_bfloat16*>(steer_vec), alpha, flag));
     return SKIPKV_OK;
