@@ -26,9 +26,9 @@
 
 namespace skipkv {
 
-constexpr int kQdWarps = 8;
+constexpr int kQdWarps = 4;
 constexpr int kQdThreads = kQdWarps * 32;
-constexpr int kQdRows = 16;                                   // rows of a tile that one warp works on
+constexpr int kQdRows = 32;                                   // rows of a tile that one warp works on: two groups of 16
 static_assert(kQdWarps * kQdRows == kQ8Tile, "a tile is a page");
 constexpr int kQdStages = 3;
 constexpr int kQdStageBytes = 2 * kQdRows * kQ8RowBytes;      // one warp's key rows, then its value rows
@@ -78,7 +78,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     const int n = Hq / Hk;                                                   // heads per group
     int* pref = reinterpret_cast<int*>(dsm + kQdRingBytes);                  // [n_slabs + 1] tile prefix
     int* lens = pref + n_slabs + 1;                                          // [n_slabs]
-    __shared__ __align__(16) float s_scale[kQdWarps][kQdStages][2];          // of the key and value rows in each stage
+    __shared__ __align__(16) float s_scale[kQdWarps][kQdStages][4];          // of each stage's key rows (two groups of 16), then of its value rows
     __shared__ float2 s_ml[kQdWarps][kMaxGroup];                             // a segment's maxima and sums
     __shared__ uint32_t s_wsum[kQdWarps];
     __shared__ __align__(8) uint64_t s_full[kQdWarps][kQdStages];            // a stage's copies have landed
@@ -114,9 +114,9 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     // parts of the tile range; divisions and the slab's tables are read once per part, a page's entry a tile ahead.
     uint8_t* const ring_p = dsm + warp * kQdStages * kQdStageBytes;
     const uint32_t ring = smem_u32(ring_p), limit = load_wait_limit(hdr);
-    const float* const sp = (lane & 1) ? c.v_scale : c.k_scale;
-    const uint32_t sp_dst = smem_u32(&s_scale[warp][0][lane & 1]);
-    const int per_tile = kQ8Tile >> c.block_log2, sub = (warp * kQdRows) >> c.block_log2;
+    const float* const sp = (lane & 2) ? c.v_scale : c.k_scale;
+    const uint32_t sp_dst = smem_u32(&s_scale[warp][0][lane & 3]);
+    const int per_tile = kQ8Tile >> c.block_log2, sub = (warp * kQdRows + (lane & 1) * 16) >> c.block_log2;
     int p_t = t_begin, p_slab = slab, p_end = t_begin, p_rows = 0, p_stage = 0;
     int p_row = 0, p_scale = 0, p_page = 0;               // row of this warp's part, place of its scale; paged: the page
     const int32_t* p_table = c.table;
@@ -146,7 +146,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             const bool in = p_row + min(p_rows, kQdRows) <= int(c.rows);
             skip &= ~(1u << p_stage);
             if (p_rows > 0 && in) {
-                // 16 rows, also where the slab has fewer left: what follows them is not used
+                // all 32 rows, also where the slab has fewer left: what follows them is not used
                 if (lane == 0) {
                     uint64_t* const bar = &s_full[warp][p_stage];
                     uint8_t* const to = ring_p + p_stage * kQdStageBytes;
@@ -154,7 +154,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     tma_load_2d(to, &k_map, 0, p_row, bar);
                     tma_load_2d(to + kQdRows * kQ8RowBytes, &v_map, 0, p_row, bar);
                 }
-                if (lane < 2) cp_async4(sp_dst + p_stage * 8, sp + p_scale);
+                if (lane < 4 && ((lane & 1) == 0 || p_rows > 16)) cp_async4(sp_dst + p_stage * 16, sp + p_scale);
             } else {
                 skip |= 1u << p_stage;
                 if (lane == 0) {
@@ -242,37 +242,52 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             if (issued < 0) issue_next();
             if (live) {
                 const uint32_t so = c_stage * kQdStageBytes;
-                const float ks = s_scale[warp][c_stage][0], vs = s_scale[warp][c_stage][1];
-                float s[2][4];                            // two chains of four steps each
+                const float4 scales = *reinterpret_cast<const float4*>(s_scale[warp][c_stage]);
+                const bool two = rows_left > 16;          // the second group has rows
+                float s[2][2][4];                         // per group two chains of four steps each
 #pragma unroll
-                for (int half = 0; half < 2; ++half) {
-                    const uint4 k0 = lds128((k_at + so) ^ (half << 4)), k1 = lds128(((k_at + so) ^ (half << 4)) + 8 * kQ8RowBytes);
-                    const uint32_t lo[4] = {k0.x, k0.y, k0.z, k0.w}, hi[4] = {k1.x, k1.y, k1.z, k1.w};
+                for (int half = 0; half < 2; ++half)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        uint32_t a0, a1, a2, a3;
-                        q8_to_f16<kFmt>(lo[i], a0, a2);
-                        q8_to_f16<kFmt>(hi[i], a1, a3);
-                        if (half == 0 && i < 2) mma16816h_first(s[i & 1], a0, a1, a2, a3, qa[4 * half + i][0], qa[4 * half + i][1]);
-                        else                    mma16816h(s[i & 1], a0, a1, a2, a3, qa[4 * half + i][0], qa[4 * half + i][1]);
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t at = ((k_at + so) ^ (half << 4)) + u * 16 * kQ8RowBytes;
+                        const uint4 k0 = lds128(at), k1 = lds128(at + 8 * kQ8RowBytes);
+                        const uint32_t lo[4] = {k0.x, k0.y, k0.z, k0.w}, hi[4] = {k1.x, k1.y, k1.z, k1.w};
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) {
+                            uint32_t a0, a1, a2, a3;
+                            q8_to_f16<kFmt>(lo[i], a0, a2);
+                            q8_to_f16<kFmt>(hi[i], a1, a3);
+                            if (half == 0 && i < 2) mma16816h_first(s[u][i & 1], a0, a1, a2, a3, qa[4 * half + i][0], qa[4 * half + i][1]);
+                            else                    mma16816h(s[u][i & 1], a0, a1, a2, a3, qa[4 * half + i][0], qa[4 * half + i][1]);
+                        }
+                    }
+                uint4 v[2][4];                            // value rows 2 qd, 2 qd + 1, 2 qd + 8, 2 qd + 9 of each group
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    v[u][0] = lds128(v_at + so + u * 16 * kQ8RowBytes); v[u][1] = lds128(v_at1 + so + u * 16 * kQ8RowBytes);
+                    v[u][2] = lds128(v_at + so + (u * 16 + 8) * kQ8RowBytes); v[u][3] = lds128(v_at1 + so + (u * 16 + 8) * kQ8RowBytes);
+                }
+                // this lane's logits: tokens g and g + 8 of either group, its two heads (packed fp32 arithmetic: a pair of heads per instruction)
+                float2 x[2], y[2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    const float f = qscale * (u ? scales.y : scales.x);
+                    const float2 f2 = make_float2(f * unshift.x, f * unshift.y);
+                    x[u] = __fmul2_rn(__fadd2_rn(make_float2(s[u][0][0], s[u][0][1]), make_float2(s[u][1][0], s[u][1][1])), f2);
+                    y[u] = __fmul2_rn(__fadd2_rn(make_float2(s[u][0][2], s[u][0][3]), make_float2(s[u][1][2], s[u][1][3])), f2);
+                }
+                if (rows_left < kQdRows) {                // the end of the slab: rows behind it hold anything, NaN too
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const int left = rows_left - 16 * u;
+                        if (g >= left) x[u] = make_float2(-INFINITY, -INFINITY);
+                        if (g + 8 >= left) y[u] = make_float2(-INFINITY, -INFINITY);
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (2 * qd + (k & 1) + (k >> 1) * 8 >= left) v[u][k] = make_uint4(0u, 0u, 0u, 0u);
                     }
                 }
-                uint4 v0 = lds128(v_at + so), v1 = lds128(v_at1 + so);
-                uint4 v2 = lds128(v_at + so + 8 * kQ8RowBytes), v3 = lds128(v_at1 + so + 8 * kQ8RowBytes);
-                // this lane's logits: tokens g and g + 8 of its two heads (packed fp32 arithmetic: a pair of heads per instruction)
-                const float f = qscale * ks;
-                const float2 f2 = make_float2(f * unshift.x, f * unshift.y);
-                float2 x = __fmul2_rn(__fadd2_rn(make_float2(s[0][0], s[0][1]), make_float2(s[1][0], s[1][1])), f2);
-                float2 y = __fmul2_rn(__fadd2_rn(make_float2(s[0][2], s[0][3]), make_float2(s[1][2], s[1][3])), f2);
-                if (rows_left < kQdRows) {                // the end of the slab: rows behind it hold anything, NaN too
-                    if (g >= rows_left) x = make_float2(-INFINITY, -INFINITY);
-                    if (g + 8 >= rows_left) y = make_float2(-INFINITY, -INFINITY);
-                    if (2 * qd >= rows_left) v0 = make_uint4(0u, 0u, 0u, 0u);
-                    if (2 * qd + 1 >= rows_left) v1 = make_uint4(0u, 0u, 0u, 0u);
-                    if (2 * qd + 8 >= rows_left) v2 = make_uint4(0u, 0u, 0u, 0u);
-                    if (2 * qd + 9 >= rows_left) v3 = make_uint4(0u, 0u, 0u, 0u);
-                }
-                float2 top = make_float2(fmaxf(x.x, y.x), fmaxf(x.y, y.y));
+                float2 top = make_float2(fmaxf(fmaxf(x[0].x, y[0].x), fmaxf(x[1].x, y[1].x)), fmaxf(fmaxf(x[0].y, y[0].y), fmaxf(x[1].y, y[1].y)));
                 if (__any_sync(0xffffffffu, top.x > m.x || top.y > m.y)) {
 #pragma unroll
                     for (int d = 4; d < 32; d <<= 1) {
@@ -288,37 +303,45 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 }
                 // 2^15 p
                 const float2 neg = make_float2(15.f - m.x, 15.f - m.y);
-                x = __fadd2_rn(x, neg); y = __fadd2_rn(y, neg);
-                x = make_float2(ex2(x.x), ex2(x.y)); y = make_float2(ex2(y.x), ex2(y.y));
-                l = __fadd2_rn(l, __fadd2_rn(x, y));
-                uint32_t hx, lx, hy, ly;
-                split_f16(x, hx, lx);
-                split_f16(y, hy, ly);
-                uint32_t ph0, ph1, pl0 = 0u, pl1 = 0u;
-                if (kFew) {
-                    const bool first = qd < 2;            // this lane's columns hold high parts (the others low ones)
-                    ph0 = movmatrix_trans(first ? hx : lx); ph1 = movmatrix_trans(first ? hy : ly);
-                } else {
-                    ph0 = movmatrix_trans(hx); ph1 = movmatrix_trans(hy);
-                    pl0 = movmatrix_trans(lx); pl1 = movmatrix_trans(ly);
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    x[u] = __fadd2_rn(x[u], neg); y[u] = __fadd2_rn(y[u], neg);
+                    x[u] = make_float2(ex2(x[u].x), ex2(x[u].y)); y[u] = make_float2(ex2(y[u].x), ex2(y[u].y));
                 }
-                const uint32_t w0[4] = {v0.x, v0.y, v0.z, v0.w}, w1[4] = {v1.x, v1.y, v1.z, v1.w};
-                const uint32_t w2[4] = {v2.x, v2.y, v2.z, v2.w}, w3[4] = {v3.x, v3.y, v3.z, v3.w};
-                const float2 vs2 = make_float2(vs, vs);
+                l = __fadd2_rn(l, __fadd2_rn(__fadd2_rn(x[0], y[0]), __fadd2_rn(x[1], y[1])));
+                uint32_t ph[2][2], pl[2][2];
+#pragma unroll
+                for (int u = 0; u < 2; ++u) {
+                    uint32_t hx, lx, hy, ly;
+                    split_f16(x[u], hx, lx);
+                    split_f16(y[u], hy, ly);
+                    if (kFew) {
+                        const bool first = qd < 2;        // this lane's columns hold high parts (the others low ones)
+                        ph[u][0] = movmatrix_trans(first ? hx : lx); ph[u][1] = movmatrix_trans(first ? hy : ly);
+                    } else {
+                        ph[u][0] = movmatrix_trans(hx); ph[u][1] = movmatrix_trans(hy);
+                        pl[u][0] = movmatrix_trans(lx); pl[u][1] = movmatrix_trans(ly);
+                    }
+                }
+                const float2 vs2[2] = {make_float2(scales.z, scales.z), two ? make_float2(scales.w, scales.w) : make_float2(0.f, 0.f)};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
+                    auto word = [&](int u, int k) { return w == 0 ? v[u][k].x : w == 1 ? v[u][k].y : w == 2 ? v[u][k].z : v[u][k].w; };
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {         // channels 16 g + 4 w + 2 u and the next; tokens 2 qd, 2 qd + 1 and 8 more
-                        const uint32_t pick = u ? 0x7362u : 0x5140u;
-                        uint32_t a0, a1, a2, a3;
-                        q8_to_f16<kFmt>(__byte_perm(w0[w], w1[w], pick), a0, a1);
-                        q8_to_f16<kFmt>(__byte_perm(w2[w], w3[w], pick), a2, a3);
-                        float d[4];
-                        mma16816h_first(d, a0, a1, a2, a3, ph0, ph1);
-                        if (!kFew) mma16816h(d, a0, a1, a2, a3, pl0, pl1);
-                        const int j = 2 * w + u;
-                        acc[j][0] = __ffma2_rn(make_float2(d[0], d[1]), vs2, acc[j][0]);
-                        acc[j][1] = __ffma2_rn(make_float2(d[2], d[3]), vs2, acc[j][1]);
+                    for (int half = 0; half < 2; ++half) {     // channels 16 g + 4 w + 2 half and the next; tokens 2 qd, 2 qd + 1 and 8 more
+                        const uint32_t pick = half ? 0x7362u : 0x5140u;
+                        const int j = 2 * w + half;
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            uint32_t a0, a1, a2, a3;
+                            q8_to_f16<kFmt>(__byte_perm(word(u, 0), word(u, 1), pick), a0, a1);
+                            q8_to_f16<kFmt>(__byte_perm(word(u, 2), word(u, 3), pick), a2, a3);
+                            float d[4];
+                            mma16816h_first(d, a0, a1, a2, a3, ph[u][0], ph[u][1]);
+                            if (!kFew) mma16816h(d, a0, a1, a2, a3, pl[u][0], pl[u][1]);
+                            acc[j][0] = __ffma2_rn(make_float2(d[0], d[1]), vs2[u], acc[j][0]);
+                            acc[j][1] = __ffma2_rn(make_float2(d[2], d[3]), vs2[u], acc[j][1]);
+                        }
                     }
                 }
             }
@@ -400,7 +423,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             if (s_last) {
                 // a warp takes a head: a lane a partial for the weights (maximum, sum) and four channels for the sums
                 const float* r0 = dec_part + size_t(fc + slab) * n * kDecPartStride;
-                constexpr int kAhead = 6;
+                constexpr int kAhead = 10;
                 const int stride = n * kDecPartStride;
 #pragma unroll 1
                 for (int hl = warp; hl < n; hl += kQdWarps) {
