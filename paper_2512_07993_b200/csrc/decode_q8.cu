@@ -34,6 +34,7 @@ constexpr int kQdStages = 3;
 constexpr int kQdStageBytes = 2 * kQdRows * kQ8RowBytes;      // one warp's key rows, then its value rows
 constexpr int kQdRingBytes = kQdWarps * kQdStages * kQdStageBytes;
 constexpr int kQdMaxGrid = 512;
+constexpr int kQdPrefetch = 3;                                // tiles that a CTA starts towards L2 before it may read the cache
 static_assert(kQdStageBytes >= kMaxGroup * kHeadDim * 4, "a warp's sums of a segment fit into a stage");
 
 // D[16 x 8] += A[16 x 16] B[16 x 8], f16 operands, fp32 accumulators; the first form has no sum to add to
@@ -92,23 +93,48 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         mbar_fence_init();
         if (warp == 0) s_abort = 0;
     }
-    pdl_wait();
-
-    // ---- schedule: CTA k has the tiles [k T / Ge, (k + 1) T / Ge) of the T tiles, Ge = the CTAs that have work
-    for (int s = tid; s < n_slabs; s += kQdThreads) lens[s] = min(max(kv_len[s], 0), q8_room(c, cap, Hk, s));
-    __syncthreads();
-    cta_prefix<kQdThreads>(n_slabs, [&](int s) { return (lens[s] + kQ8Tile - 1) / kQ8Tile; }, pref, s_wsum);
-    const int T = pref[n_slabs], Ge = min(G, T);
-    const int t_begin = cta < Ge ? int((long long)cta * T / Ge) : T, t_end = cta < Ge ? int((long long)(cta + 1) * T / Ge) : T;
-    int slab = 0;
-    {
+    // ---- schedule: CTA k has the tiles [k T / Ge, (k + 1) T / Ge) of the T tiles, Ge = the CTAs that have work.  The lengths may be written by
+    // the launch ahead of this one, but the number of tiles they make is mostly older (a step adds one row).  So the schedule is derived from what
+    // they are now, the CTA's first tiles are started towards L2 (the point of coherence, so a row that is still being written is not read too
+    // early), and behind the wait the first copies go out under it at once; the lengths and the first row are read once more while those are on
+    // their way, and only if the schedule is another one is it derived again.  (These reads bypass L1, which could keep the earlier value.)
+    const int s_per = (n_slabs + kQdThreads - 1) / kQdThreads;
+    const int s_lo = min(tid * s_per, n_slabs), s_hi = min(s_lo + s_per, n_slabs);
+    auto length = [&](int s) { return min(max(__ldcg(kv_len + s), 0), q8_room(c, cap, Hk, s)); };
+    auto tiles = [](int rows) { return (rows + kQ8Tile - 1) / kQ8Tile; };
+#pragma unroll 1
+    for (int s = s_lo; s < s_hi; ++s) lens[s] = length(s);
+    int T, Ge, t_begin, t_end, slab;
+    auto derive = [&]() {
+        cta_prefix<kQdThreads>(n_slabs, [&](int s) { return tiles(lens[s]); }, pref, s_wsum);
+        T = pref[n_slabs];
+        Ge = min(G, T);
+        t_begin = cta < Ge ? int((long long)cta * T / Ge) : T;
+        t_end = cta < Ge ? int((long long)(cta + 1) * T / Ge) : T;
+        slab = 0;
         int hi = n_slabs - 1;                             // slab holding tile t_begin: the last one with pref <= t_begin
         while (slab < hi) {
             const int mid = (slab + hi + 1) >> 1;
             if (pref[mid] <= t_begin) slab = mid; else hi = mid - 1;
         }
+    };
+    derive();
+    // first row of the first slab; paged: the page of the CTA's first tile
+    auto first_row = [&]() {
+        if (t_begin >= t_end) return 0ll;
+        if (c.table) return (long long)__ldcg(c.table + size_t(slab) * c.max_pages + (t_begin - pref[slab]));
+        return (long long)(__ldcg(reinterpret_cast<const long long*>(slab_off) + slab / Hk) * Hk + (long long)(slab % Hk) * __ldcg(cap + slab / Hk));
+    };
+    long long row_first = first_row();
+    if (tid < 2 * kQdPrefetch && t_begin + (tid >> 1) < min(t_end, pref[slab + 1])) {
+        const int t = t_begin + (tid >> 1), j = t - pref[slab], rows = min(lens[slab] - j * kQ8Tile, kQ8Tile);
+        const long long row = !c.table ? row_first + (long long)j * kQ8Tile
+                                       : (t == t_begin ? row_first : (long long)__ldcg(c.table + size_t(slab) * c.max_pages + j)) * kQ8Tile;
+        if (row >= 0 && row + rows <= c.rows)
+            asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(((tid & 1) ? c.V : c.K) + row * kQ8RowBytes), "r"(rows * kQ8RowBytes) : "memory");
     }
-    pdl_trigger();
+    if (tid < 2) tmap_prefetch(tid ? &v_map : &k_map);
+    pdl_wait();
 
     // ---- copies: this warp's 16 rows of the CTA's k-th tile, and their two scales, go to stage k % kQdStages.  The cursor walks the slab
     // parts of the tile range; divisions and the slab's tables are read once per part, a page's entry a tile ahead.
@@ -117,11 +143,14 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     const float* const sp = (lane & 2) ? c.v_scale : c.k_scale;
     const uint32_t sp_dst = smem_u32(&s_scale[warp][0][lane & 3]);
     const int per_tile = kQ8Tile >> c.block_log2, sub = (warp * kQdRows + (lane & 1) * 16) >> c.block_log2;
-    int p_t = t_begin, p_slab = slab, p_end = t_begin, p_rows = 0, p_stage = 0;
+    int p_t = t_begin, p_slab = slab, p_end = t_begin, p_rows = 0, p_stage = 0, fills = 0;
     int p_row = 0, p_scale = 0, p_page = 0;               // row of this warp's part, place of its scale; paged: the page
     const int32_t* p_table = c.table;
+    const int all_scales = c.table ? 0x7fffffff : n_slabs * c.max_blocks;
     uint32_t skip = 0;                                    // stages without copies: no rows, or rows that lie outside the buffers
-    auto issue_next = [&]() {
+    bool far = false;                                     // a copy was left out under the schedule from before the wait
+    // early: under that schedule, with a length that may be old: all of the tile is copied
+    auto issue_next = [&](bool early) {
         if (p_t < t_end) {
             if (p_t == p_end) {
                 while (pref[p_slab + 1] <= p_t) ++p_slab;
@@ -130,9 +159,9 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 p_rows = lens[p_slab] - j * kQ8Tile - warp * kQdRows;
                 if (c.table) {
                     p_table = c.table + size_t(p_slab) * c.max_pages + j;
-                    p_page = *p_table;
+                    p_page = p_t == t_begin ? int(row_first) : __ldcg(p_table);
                 } else {
-                    const long long row0 = (long long)slab_row0(slab_off, cap, Hk, p_slab / Hk, p_slab % Hk);
+                    const long long row0 = p_t == t_begin ? row_first : (long long)slab_row0(slab_off, cap, Hk, p_slab / Hk, p_slab % Hk);
                     p_row = int(row0 < 0 ? c.rows : min(row0 + (long long)j * kQ8Tile + warp * kQdRows, c.rows));
                     p_scale = p_slab * c.max_blocks + j * per_tile + sub;
                 }
@@ -141,12 +170,13 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 const bool in = uint32_t(p_page) < uint32_t(c.rows / kQ8Tile);
                 p_row = in ? p_page * kQ8Tile + warp * kQdRows : int(c.rows);
                 p_scale = in ? p_page * per_tile + sub : 0;
-                if (p_t + 1 < p_end) p_page = *++p_table;
+                if (p_t + 1 < p_end) p_page = __ldcg(++p_table);
             }
+            const int rows = early ? kQdRows : min(p_rows, kQdRows);
             const bool in = p_row + min(p_rows, kQdRows) <= int(c.rows);
             skip &= ~(1u << p_stage);
-            if (p_rows > 0 && in) {
-                // all 32 rows, also where the slab has fewer left: what follows them is not used
+            if (rows > 0 && in && p_row < int(c.rows)) {
+                // all 32 rows, also where the slab has fewer left: what follows them is not used (zeros behind the buffer)
                 if (lane == 0) {
                     uint64_t* const bar = &s_full[warp][p_stage];
                     uint8_t* const to = ring_p + p_stage * kQdStageBytes;
@@ -154,25 +184,57 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     tma_load_2d(to, &k_map, 0, p_row, bar);
                     tma_load_2d(to + kQdRows * kQ8RowBytes, &v_map, 0, p_row, bar);
                 }
-                if (lane < 4 && ((lane & 1) == 0 || p_rows > 16)) cp_async4(sp_dst + p_stage * 16, sp + p_scale);
+                if (lane < 4 && ((lane & 1) == 0 || rows > 16)) cp_async4(sp_dst + p_stage * 16, sp + min(p_scale, all_scales - 1));
             } else {
                 skip |= 1u << p_stage;
+                far = far || (early && !in);
                 if (lane == 0) {
                     mbar_arrive(&s_full[warp][p_stage]);
-                    if (p_rows > 0) atomicOr(&hdr->status, SKIPKV_STATUS_BAD_TABLE);
+                    if (rows > 0 && !early) atomicOr(&hdr->status, SKIPKV_STATUS_BAD_TABLE);
                 }
             }
             p_rows -= kQ8Tile;
             p_row = min(p_row + kQ8Tile, int(c.rows));
             p_scale += per_tile;
             ++p_t;
+            ++fills;
             if (++p_stage == kQdStages) p_stage = 0;
         }
         cp_async_commit();                                // (of the scales; empty groups keep the count)
     };
     __syncwarp();
+    const int len_again = s_lo < s_hi ? length(s_lo) : 0;
+    const long long row_again = first_row();
+    int issued = -1, c_stage = 0;                         // issued: copies that were started when a wait gave up
 #pragma unroll 1
-    for (int k = 0; k < kQdStages - 1; ++k) issue_next();
+    for (int attempt = 0;; ++attempt) {
+#pragma unroll 1
+        for (int k = 0; k < kQdStages - 1; ++k) issue_next(attempt == 0);
+        if (attempt) break;
+        int changed = row_again != row_first || far;
+#pragma unroll 1
+        for (int s = s_lo; s < s_hi; ++s) {
+            const int now = s == s_lo ? len_again : length(s);
+            if (now == lens[s]) continue;
+            // (a slab that now reaches beyond the buffer is left to the checks of the second attempt)
+            if (tiles(now) != tiles(lens[s]) || (!c.table && (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk) + now > c.rows)) changed = 1;
+            lens[s] = now;
+        }
+        if (!__syncthreads_or(changed)) {
+            if (p_t < p_end) p_rows = lens[p_slab] - (p_t - pref[p_slab]) * kQ8Tile - warp * kQdRows;      // (a length within its last tile)
+            break;
+        }
+        // another schedule: what is on its way is waited for and left
+        cp_async_wait<0>();
+        for (int k = 0; k < fills && issued < 0; ++k)
+            if (!warp_wait(&s_full[warp][k], 0u, limit, &s_abort, &hdr->status)) issued = fills;
+        derive();
+        row_first = first_row();
+        p_t = p_end = t_begin; p_slab = slab;
+        c_stage = p_stage;
+        if (issued >= 0) p_t = p_end = t_end;             // (a wait gave up: no more copies)
+    }
+    pdl_trigger();
 
     {
         const int side0 = (warp * G + cta) * 32 + lane, side_step = G * kQdThreads;
@@ -220,8 +282,8 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     const uint32_t v_at = ring + (kQdRows + 2 * qd) * kQ8RowBytes + ((g ^ (2 * qd)) << 4);
     const uint32_t v_at1 = (v_at ^ 16u) + kQ8RowBytes;
 
-    int t = t_begin, c_stage = 0, issued = -1;            // issued: tiles whose copies were started when a wait gave up
-    uint32_t parity = 0;
+    int t = t_begin;
+    uint32_t parity = 0;                                  // (of the stage's copies: a discarded first round moves on the stage, never past the last)
     while (t < t_end) {
         // -------------------------------------------------------------- one (CTA, slab) segment
         while (pref[slab + 1] <= t) ++slab;
@@ -237,9 +299,9 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         for (; t < seg_end; ++t, rows_left -= kQ8Tile) {
             cp_async_wait<kQdStages - 2>();
             const bool landed = warp_wait(&s_full[warp][c_stage], parity, limit, &s_abort, &hdr->status);
-            if (!landed && issued < 0) issued = p_t - t_begin;       // from here on this warp copies nothing and works on nothing
-            const bool live = issued < 0 && !((skip >> c_stage) & 1u);
-            if (issued < 0) issue_next();
+            if (!landed && issued < 0) issued = fills;        // from here on this warp copies nothing and works on nothing
+            const bool live = issued < 0 && rows_left > 0 && !((skip >> c_stage) & 1u);
+            if (issued < 0) issue_next(false);
             if (live) {
                 const uint32_t so = c_stage * kQdStageBytes;
                 const float4 scales = *reinterpret_cast<const float4*>(s_scale[warp][c_stage]);
