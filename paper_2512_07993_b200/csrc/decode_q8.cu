@@ -34,8 +34,11 @@ constexpr int kQdStages = 3;
 constexpr int kQdStageBytes = 2 * kQdRows * kQ8RowBytes;      // one warp's key rows, then its value rows
 constexpr int kQdRingBytes = kQdWarps * kQdStages * kQdStageBytes;
 constexpr int kQdMaxGrid = 512;
+constexpr int kQdPartCost = 4;                                // what a slab costs beside its tiles, in tiles: the end of a part
 constexpr int kQdPrefetch = 3;                                // tiles that a CTA starts towards L2 before it may read the cache
-static_assert(kQdStageBytes >= kMaxGroup * kHeadDim * 4, "a warp's sums of a segment fit into a stage");
+constexpr int kQdSumStride = kHeadDim + 4;                    // (of a column's sums in shared memory)
+static_assert(kQdStageBytes >= 8 * kQdSumStride * 4, "a warp's sums of a segment fit into a stage");
+static_assert(kQdThreads == kHeadDim, "a thread merges one channel");
 
 // D[16 x 8] += A[16 x 16] B[16 x 8], f16 operands, fp32 accumulators; the first form has no sum to add to
 __device__ __forceinline__ void mma16816h(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
@@ -106,32 +109,37 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     for (int s = s_lo; s < s_hi; ++s) lens[s] = length(s);
     int T, Ge, t_begin, t_end, slab;
     auto derive = [&]() {
-        cta_prefix<kQdThreads>(n_slabs, [&](int s) { return tiles(lens[s]); }, pref, s_wsum);
+        cta_prefix<kQdThreads>(n_slabs, [&](int s) { return lens[s] ? tiles(lens[s]) + kQdPartCost : 0; }, pref, s_wsum);
         T = pref[n_slabs];
         Ge = min(G, T);
         t_begin = cta < Ge ? int((long long)cta * T / Ge) : T;
         t_end = cta < Ge ? int((long long)(cta + 1) * T / Ge) : T;
         slab = 0;
-        int hi = n_slabs - 1;                             // slab holding tile t_begin: the last one with pref <= t_begin
+        int hi = n_slabs - 1;                             // slab holding place t_begin: the last one with pref <= t_begin
         while (slab < hi) {
             const int mid = (slab + hi + 1) >> 1;
             if (pref[mid] <= t_begin) slab = mid; else hi = mid - 1;
         }
+        t_begin = max(t_begin, pref[slab] + kQdPartCost);
     };
     derive();
+    auto cta_of = [&](int place) { return int(((long long)(place + 1) * Ge - 1) / T); };
     // first row of the first slab; paged: the page of the CTA's first tile
     auto first_row = [&]() {
         if (t_begin >= t_end) return 0ll;
-        if (c.table) return (long long)__ldcg(c.table + size_t(slab) * c.max_pages + (t_begin - pref[slab]));
+        if (c.table) return (long long)__ldcg(c.table + size_t(slab) * c.max_pages + (t_begin - pref[slab] - kQdPartCost));
         return (long long)(__ldcg(reinterpret_cast<const long long*>(slab_off) + slab / Hk) * Hk + (long long)(slab % Hk) * __ldcg(cap + slab / Hk));
     };
     long long row_first = first_row();
     if (tid < 2 * kQdPrefetch && t_begin + (tid >> 1) < min(t_end, pref[slab + 1])) {
-        const int t = t_begin + (tid >> 1), j = t - pref[slab], rows = min(lens[slab] - j * kQ8Tile, kQ8Tile);
+        const int t = t_begin + (tid >> 1), j = t - pref[slab] - kQdPartCost, rows = min(lens[slab] - j * kQ8Tile, kQ8Tile);
         const long long row = !c.table ? row_first + (long long)j * kQ8Tile
                                        : (t == t_begin ? row_first : (long long)__ldcg(c.table + size_t(slab) * c.max_pages + j)) * kQ8Tile;
-        if (row >= 0 && row + rows <= c.rows)
+        if (row >= 0 && row + rows <= c.rows) {
             asm volatile("cp.async.bulk.prefetch.L2.global [%0], %1;" ::"l"(((tid & 1) ? c.V : c.K) + row * kQ8RowBytes), "r"(rows * kQ8RowBytes) : "memory");
+            const size_t at = c.table ? size_t(row / kQ8Tile) * (kQ8Tile >> c.block_log2) : size_t(slab) * c.max_blocks + size_t(j) * (kQ8Tile >> c.block_log2);
+            asm volatile("prefetch.global.L2 [%0];" ::"l"(((tid & 1) ? c.v_scale : c.k_scale) + at));
+        }
     }
     if (tid < 2) tmap_prefetch(tid ? &v_map : &k_map);
     pdl_wait();
@@ -155,7 +163,9 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             if (p_t == p_end) {
                 while (pref[p_slab + 1] <= p_t) ++p_slab;
                 p_end = pref[p_slab + 1];
-                const int j = p_t - pref[p_slab];
+                p_t = max(p_t, pref[p_slab] + kQdPartCost);
+                if (p_t >= t_end) { p_t = p_end = t_end; cp_async_commit(); return; }
+                const int j = p_t - pref[p_slab] - kQdPartCost;
                 p_rows = lens[p_slab] - j * kQ8Tile - warp * kQdRows;
                 if (c.table) {
                     p_table = c.table + size_t(p_slab) * c.max_pages + j;
@@ -203,6 +213,20 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         cp_async_commit();                                // (of the scales; empty groups keep the count)
     };
     __syncwarp();
+    // What else comes from memory before the first tile is requested here and consumed behind the first copies.
+    const int g = lane >> 2, qd = lane & 3;               // mma fragments: rows (tokens, channels) g and g + 8, columns (heads) 2 qd and 2 qd + 1
+    uint32_t qa[8][2];
+    auto fetch_q = [&](int slab_) {                       // a slab's queries: head g (few: g & 3), channels 32 qd to 32 qd + 31
+        const int hd = kFew ? g & 3 : g;
+        const uint4* qp = reinterpret_cast<const uint4*>(q + (size_t(slab_) * n + min(hd, n - 1)) * kHeadDim + qd * 32);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint4 v = hd < n ? qp[i] : make_uint4(0u, 0u, 0u, 0u);
+            qa[2 * i][0] = v.x; qa[2 * i][1] = v.y; qa[2 * i + 1][0] = v.z; qa[2 * i + 1][1] = v.w;
+        }
+    };
+    int q_slab = slab;
+    if (t_begin < t_end) fetch_q(slab);
     const int len_again = s_lo < s_hi ? length(s_lo) : 0;
     const long long row_again = first_row();
     int issued = -1, c_stage = 0;                         // issued: copies that were started when a wait gave up
@@ -221,7 +245,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             lens[s] = now;
         }
         if (!__syncthreads_or(changed)) {
-            if (p_t < p_end) p_rows = lens[p_slab] - (p_t - pref[p_slab]) * kQ8Tile - warp * kQdRows;      // (a length within its last tile)
+            if (p_t < p_end) p_rows = lens[p_slab] - (p_t - pref[p_slab] - kQdPartCost) * kQ8Tile - warp * kQdRows;      // (a length within its last tile)
             break;
         }
         // another schedule: what is on its way is waited for and left
@@ -232,6 +256,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         row_first = first_row();
         p_t = p_end = t_begin; p_slab = slab;
         c_stage = p_stage;
+        q_slab = -1;
         if (issued >= 0) p_t = p_end = t_end;             // (a wait gave up: no more copies)
     }
     pdl_trigger();
@@ -244,20 +269,11 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             steer_store(i, vec_per_row, hidden, steer_load(i, vec_per_row, hidden, steer_vec, alpha, flag));
     }
 
-    const int g = lane >> 2, qd = lane & 3;               // mma fragments: rows (tokens, channels) g and g + 8, columns (heads) 2 qd and 2 qd + 1
-    // Queries of a slab: column g (head) of the B operand, channels 32 qd + 4 ks + {0, 1} and {2, 3} in step ks, times 2^shift; unshift
-    // takes the two heads of the accumulator's columns back.
-    uint32_t qa[8][2];
+    // The B operand: column g (head), channels 32 qd + 4 ks + {0, 1} and {2, 3} in step ks, times 2^shift; unshift takes the two heads of the
+    // accumulator's columns back.
     float2 unshift = make_float2(1.f, 1.f);
-    auto load_q = [&](int slab_) {
-        const int hd = kFew ? g & 3 : g;                  // head of this lane's column
-        const uint4* qp = reinterpret_cast<const uint4*>(q + (size_t(slab_ / Hk) * Hq + size_t(slab_ % Hk) * n + min(hd, n - 1)) * kHeadDim + qd * 32);
+    auto shift_q = [&]() {
         uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint4 v = hd < n ? qp[i] : make_uint4(0u, 0u, 0u, 0u);
-            qa[2 * i][0] = v.x; qa[2 * i][1] = v.y; qa[2 * i + 1][0] = v.z; qa[2 * i + 1][1] = v.w;
-        }
 #pragma unroll
         for (int i = 0; i < 8; ++i) m = __vmaxu2(m, __vmaxu2(qa[i][0] & 0x7fff7fffu, qa[i][1] & 0x7fff7fffu));
         m = max(m & 0xffffu, m >> 16);
@@ -282,19 +298,32 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     const uint32_t v_at = ring + (kQdRows + 2 * qd) * kQ8RowBytes + ((g ^ (2 * qd)) << 4);
     const uint32_t v_at1 = (v_at ^ 16u) + kQ8RowBytes;
 
+    // a warp's sums of a segment lie in the stage of its last tile
+    auto sums = [&](int w) { return reinterpret_cast<float*>(dsm + (size_t(w) * kQdStages + (c_stage == 0 ? kQdStages - 1 : c_stage - 1)) * kQdStageBytes); };
     int t = t_begin;
     uint32_t parity = 0;                                  // (of the stage's copies: a discarded first round moves on the stage, never past the last)
-    while (t < t_end) {
+    // The slab whose part this CTA has delivered, and the answer to its arrival, which nothing waits for before the next part is worked on.
+    int pend = -1, pend_parts = 0, pend_cta = 0;
+    uint32_t pend_old = 0;
+    while (true) {
         // -------------------------------------------------------------- one (CTA, slab) segment
-        while (pref[slab + 1] <= t) ++slab;
+        while (t < t_end && pref[slab + 1] <= t) ++slab;
+        if (t < t_end) t = max(t, pref[slab] + kQdPartCost);
+        const bool more = t < t_end;
+        if (!more && pend < 0) break;
+        int n_part = 0, first_cta = 0;
+        if (more) {
         const int seg_end = min(t_end, pref[slab + 1]);
-        const int b = slab / Hk, h = slab % Hk;
-        load_q(slab);
+        first_cta = cta_of(pref[slab] + kQdPartCost);
+        n_part = cta_of(pref[slab + 1] - 1) - first_cta + 1;
+        if (slab != q_slab) { fetch_q(slab); q_slab = slab; }
+        shift_q();
+        q_slab = -1;
         float2 acc[8][2];                                 // channels 16 g + 2 j and 16 g + 2 j + 1 of the lane's two heads
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j][0] = acc[j][1] = make_float2(0.f, 0.f);
         float2 m = make_float2(-INFINITY, -INFINITY), l = make_float2(0.f, 0.f);    // their running maximum, this lane's share of the sum
-        int rows_left = lens[slab] - (t - pref[slab]) * kQ8Tile - warp * kQdRows;     // of this warp's part of the tile
+        int rows_left = lens[slab] - (t - pref[slab] - kQdPartCost) * kQ8Tile - warp * kQdRows;     // of this warp's part of the tile
 #pragma unroll 1
         for (; t < seg_end; ++t, rows_left -= kQ8Tile) {
             cp_async_wait<kQdStages - 2>();
@@ -411,80 +440,72 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             if (++c_stage == kQdStages) { c_stage = 0; parity ^= 1u; }
         }
 
-        // -------------------------------------------------------------- flush this (CTA, slab) segment
+        // -------------------------------------------------------------- the end of a segment
 #pragma unroll
         for (int d = 4; d < 32; d <<= 1) {
             l.x += __shfl_xor_sync(0xffffffffu, l.x, d);
             l.y += __shfl_xor_sync(0xffffffffu, l.y, d);
         }
-        if (kFew) {                                       // the same heads' low parts
+        // The columns' sums (few: high and low parts apart) go to the stage of the tile that was worked on last: its rows are read out, and the
+        // next copy into it is issued behind the barriers below.
+        {
+            float* wp = sums(warp) + size_t(2 * qd) * kQdSumStride + 16 * g;
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    acc[j][k].x += __shfl_xor_sync(0xffffffffu, acc[j][k].x, 2);
-                    acc[j][k].y += __shfl_xor_sync(0xffffffffu, acc[j][k].y, 2);
-                }
-        }
-        // The sums go to the stage of the tile that was worked on last: its rows are read out, and the next copy into it is issued behind the
-        // barriers below.
-        const int free_stage = c_stage == 0 ? kQdStages - 1 : c_stage - 1;
-        auto sums = [&](int w) { return reinterpret_cast<float*>(dsm + (size_t(w) * kQdStages + free_stage) * kQdStageBytes); };
-        if (!kFew || qd < 2) {
-            float* wp = sums(warp) + size_t(2 * qd) * kHeadDim + 16 * g;
-            if (2 * qd < n) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    reinterpret_cast<float4*>(wp)[j] = make_float4(acc[2 * j][0].x, acc[2 * j][1].x, acc[2 * j + 1][0].x, acc[2 * j + 1][1].x);
-                if (g == 0) s_ml[warp][2 * qd] = make_float2(m.x, l.x);
+            for (int j = 0; j < 4; ++j) {
+                reinterpret_cast<float4*>(wp)[j] = make_float4(acc[2 * j][0].x, acc[2 * j][1].x, acc[2 * j + 1][0].x, acc[2 * j + 1][1].x);
+                reinterpret_cast<float4*>(wp + kQdSumStride)[j] = make_float4(acc[2 * j][0].y, acc[2 * j][1].y, acc[2 * j + 1][0].y, acc[2 * j + 1][1].y);
             }
-            wp += kHeadDim;
-            if (2 * qd + 1 < n) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-                    reinterpret_cast<float4*>(wp)[j] = make_float4(acc[2 * j][0].y, acc[2 * j][1].y, acc[2 * j + 1][0].y, acc[2 * j + 1][1].y);
-                if (g == 0) s_ml[warp][2 * qd + 1] = make_float2(m.y, l.y);
-            }
+            if (g == 0) { s_ml[warp][2 * qd] = make_float2(m.x, l.x); s_ml[warp][2 * qd + 1] = make_float2(m.y, l.y); }
         }
-        fence_proxy_async_smem();                         // (the stage's next writer is a bulk copy)
+        if (t < t_end) fence_proxy_async_smem();          // (the stage's next writer is a bulk copy)
+        }
+        if (pend >= 0 && tid == 0) {
+            const int last = pend_old == uint32_t(pend_parts - 1) ? 1 : 0;
+            if (last) dec_cnt[pend] = 0u;                 // self-resetting for the next launch
+            s_last = last;
+        }
         __syncthreads();
-        // merge the warps; thread -> channel of every other head
-        const int fc = int(((long long)(pref[slab] + 1) * Ge - 1) / T), lc = int(((long long)pref[slab + 1] * Ge - 1) / T);
-        const int n_part = lc - fc + 1;
-        __nv_bfloat16* o = out + (size_t(b) * Hq + size_t(h) * n) * kHeadDim;
-        float* rec = dec_part + size_t(cta + slab) * n * kDecPartStride;
-        const int ch = tid & (kHeadDim - 1);
+        const bool last = pend >= 0 && s_last;
+        const int done = pend, done_parts = pend_parts, done_cta = pend_cta;
+        pend = -1;
+        if (more) {
+            // merge the warps; thread -> channel
+            __nv_bfloat16* o = out + size_t(slab) * n * kHeadDim;
+            float* rec = dec_part + size_t(cta + slab) * n * kDecPartStride;
 #pragma unroll 1
-        for (int hl = tid / kHeadDim; hl < n; hl += kQdThreads / kHeadDim) {
-            float M = -1e30f, L = 0.f, A = 0.f;           // (finite: a warp without rows has -inf)
+            for (int hl = 0; hl < n; ++hl) {
+                float M = -1e30f, L = 0.f, A = 0.f;       // (finite: a warp without rows has -inf)
 #pragma unroll
-            for (int w = 0; w < kQdWarps; ++w) M = fmaxf(M, s_ml[w][hl].x);
+                for (int w = 0; w < kQdWarps; ++w) M = fmaxf(M, s_ml[w][hl].x);
 #pragma unroll
-            for (int w = 0; w < kQdWarps; ++w) {
-                const float2 ml = s_ml[w][hl];
-                const float e = ex2(ml.x - M);
-                L = fmaf(ml.y, e, L);
-                A = fmaf(sums(w)[hl * kHeadDim + ch], e, A);
+                for (int w = 0; w < kQdWarps; ++w) {
+                    const float2 ml = s_ml[w][hl];
+                    const float e = ex2(ml.x - M);
+                    const float* p = sums(w) + hl * kQdSumStride + tid;
+                    L = fmaf(ml.y, e, L);
+                    A = fmaf(kFew ? p[0] + p[4 * kQdSumStride] : p[0], e, A);
+                }
+                if (n_part == 1) {
+                    o[hl * kHeadDim + tid] = __float2bfloat16_rn(L == 0.f ? 0.f : A / L);
+                } else {
+                    rec[hl * kDecPartStride + tid] = A;
+                    if (tid == 0) *reinterpret_cast<float2*>(rec + hl * kDecPartStride + kHeadDim) = make_float2(M, L);
+                }
             }
-            if (n_part == 1) {
-                o[hl * kHeadDim + ch] = __float2bfloat16_rn(L == 0.f ? 0.f : A / L);
-            } else {
-                rec[hl * kDecPartStride + ch] = A;
-                if (ch == 0) *reinterpret_cast<float2*>(rec + hl * kDecPartStride + kHeadDim) = make_float2(M, L);
+            __syncthreads();                              // every thread's record stores are ordered before the arrival; the sums are read
+            if (n_part > 1) {
+                pend = slab;
+                pend_parts = n_part;
+                pend_cta = first_cta;
+                if (tid == 0) pend_old = arrive_acq_rel(dec_cnt + slab);
             }
         }
-        __syncthreads();                                  // every thread's record stores are ordered before the arrival; the sums are read
-        if (n_part > 1) {
-            if (tid == 0) {
-                const uint32_t old = arrive_acq_rel(dec_cnt + slab);
-                const int last = (old == uint32_t(n_part - 1)) ? 1 : 0;
-                if (last) dec_cnt[slab] = 0u;             // self-resetting for the next launch
-                s_last = last;
-            }
-            __syncthreads();
-            if (s_last) {
+        if (last) {
+            {
                 // a warp takes a head: a lane a partial for the weights (maximum, sum) and four channels for the sums
-                const float* r0 = dec_part + size_t(fc + slab) * n * kDecPartStride;
+                const int n_part = done_parts;
+                const float* r0 = dec_part + size_t(done_cta + done) * n * kDecPartStride;
+                __nv_bfloat16* o = out + size_t(done) * n * kHeadDim;
                 constexpr int kAhead = 10;
                 const int stride = n * kDecPartStride;
 #pragma unroll 1
@@ -543,7 +564,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
 #pragma unroll 1
     for (int s = cta; s < n_slabs; s += G) {
         if (lens[s]) continue;
-        __nv_bfloat16* o = out + (size_t(s / Hk) * Hq + size_t(s % Hk) * n) * kHeadDim;
+        __nv_bfloat16* o = out + size_t(s) * n * kHeadDim;
 #pragma unroll 1
         for (int i = tid; i < n * kHeadDim; i += kQdThreads) o[i] = __float2bfloat16_rn(0.f);
     }
