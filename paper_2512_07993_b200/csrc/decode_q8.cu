@@ -38,6 +38,9 @@ constexpr int kQdPartCost = 4;                                // what a slab cos
 constexpr int kQdPrefetch = 3;                                // tiles that a CTA starts towards L2 before it may read the cache
 constexpr int kQdSumStride = kHeadDim + 4;                    // (of a column's sums in shared memory)
 static_assert(kQdStageBytes >= 8 * kQdSumStride * 4, "a warp's sums of a segment fit into a stage");
+constexpr int kQdMergeParts = kQdStageBytes / (kHeadDim * 4);   // partials of a head that are merged at a time
+static_assert(kQdMergeParts == 16, "half a warp");
+static_assert((1ull << 22) * kQdMaxGrid <= (1ull << 32), "places times CTAs in 32 bits");
 static_assert(kQdThreads == kHeadDim, "a thread merges one channel");
 
 // D[16 x 8] += A[16 x 16] B[16 x 8], f16 operands, fp32 accumulators; the first form has no sum to add to
@@ -112,8 +115,9 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         cta_prefix<kQdThreads>(n_slabs, [&](int s) { return lens[s] ? tiles(lens[s]) + kQdPartCost : 0; }, pref, s_wsum);
         T = pref[n_slabs];
         Ge = min(G, T);
-        t_begin = cta < Ge ? int((long long)cta * T / Ge) : T;
-        t_end = cta < Ge ? int((long long)(cta + 1) * T / Ge) : T;
+        auto first_of = [&](int k) { return T < (1 << 22) ? int(uint32_t(k) * uint32_t(T) / uint32_t(Ge)) : int((long long)k * T / Ge); };
+        t_begin = cta < Ge ? first_of(cta) : T;
+        t_end = cta < Ge ? first_of(cta + 1) : T;
         slab = 0;
         int hi = n_slabs - 1;                             // slab holding place t_begin: the last one with pref <= t_begin
         while (slab < hi) {
@@ -123,7 +127,9 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         t_begin = max(t_begin, pref[slab] + kQdPartCost);
     };
     derive();
-    auto cta_of = [&](int place) { return int(((long long)(place + 1) * Ge - 1) / T); };
+    auto cta_of = [&](int place) {
+        return T < (1 << 22) ? int((uint32_t(place + 1) * uint32_t(Ge) - 1u) / uint32_t(T)) : int(((long long)(place + 1) * Ge - 1) / T);
+    };
     // first row of the first slab; paged: the page of the CTA's first tile
     auto first_row = [&]() {
         if (t_begin >= t_end) return 0ll;
@@ -501,58 +507,51 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             }
         }
         if (last) {
-            {
-                // a warp takes a head: a lane a partial for the weights (maximum, sum) and four channels for the sums
-                const int n_part = done_parts;
-                const float* r0 = dec_part + size_t(done_cta + done) * n * kDecPartStride;
-                __nv_bfloat16* o = out + size_t(done) * n * kHeadDim;
-                constexpr int kAhead = 10;
-                const int stride = n * kDecPartStride;
+            // This CTA was the last to deliver a part of slab `done`: a warp takes a head, a lane a partial for the weights (maximum, sum) and four
+            // channels for the sums.  They come through shared memory (the warp's stage that is read out), so that all are on their way at once.
+            const float* r0 = dec_part + size_t(done_cta + done) * n * kDecPartStride;
+            const size_t stride = size_t(n) * kDecPartStride;
+            float* const to = sums(warp) + lane * 4;
 #pragma unroll 1
-                for (int hl = warp; hl < n; hl += kQdWarps) {
-                    const float* rh = r0 + hl * kDecPartStride;
-                    float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
-                    float M = -1e30f, L = 0.f;
+            for (int hl = warp; hl < n; hl += kQdWarps) {
+                const float* rh = r0 + hl * kDecPartStride;
+                float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
+                float M = -1e30f, L = 0.f;
 #pragma unroll 1
-                    for (int p0 = 0; p0 < n_part; p0 += 32) {
-                        const int cnt = min(32, n_part - p0);
-                        const bool on = lane < cnt;
-                        const float2 ml = __ldcg(reinterpret_cast<const float2*>(rh + size_t((p0 + min(lane, cnt - 1)) * stride) + kHeadDim));
-                        float4 a[kAhead];
+                for (int p0 = 0; p0 < done_parts; p0 += kQdMergeParts) {
+                    const int cnt = min(kQdMergeParts, done_parts - p0);
+                    const bool on = lane < cnt;
+                    const float2 ml = __ldcg(reinterpret_cast<const float2*>(rh + size_t(p0 + min(lane, cnt - 1)) * stride + kHeadDim));
+#pragma unroll 4
+                    for (int k = 0; k < cnt; ++k) cp_async16(smem_u32(to + k * kHeadDim), rh + size_t(p0 + k) * stride + lane * 4);
+                    cp_async_commit();
+                    float mx = on ? ml.x : -INFINITY;
 #pragma unroll
-                        for (int k = 0; k < kAhead; ++k)
-                            if (k < cnt) a[k] = __ldcg(reinterpret_cast<const float4*>(rh + size_t((p0 + k) * stride)) + lane);
-                        float mx = on ? ml.x : -INFINITY;
+                    for (int d = kQdMergeParts / 2; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
+                    mx = __shfl_sync(0xffffffffu, mx, 0);
+                    const float Mn = fmaxf(M, mx), keep = ex2(M - Mn);
+                    const float w = on ? ex2(ml.x - Mn) : 0.f;
+                    float ls = on ? ml.y * w : 0.f;
 #pragma unroll
-                        for (int d = 16; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
-                        const float Mn = fmaxf(M, mx), keep = ex2(M - Mn);
-                        const float w = on ? ex2(ml.x - Mn) : 0.f;
-                        float ls = on ? ml.y * w : 0.f;
-#pragma unroll
-                        for (int d = 16; d; d >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, d);
-                        L = fmaf(L, keep, ls);
-                        M = Mn;
-                        A.x *= keep; A.y *= keep; A.z *= keep; A.w *= keep;
-#pragma unroll 1
-                        for (int k0 = 0; k0 < cnt; k0 += kAhead) {
-#pragma unroll
-                            for (int k = 0; k < kAhead; ++k)
-                                if (k0 + k < cnt) {
-                                    const float wk = __shfl_sync(0xffffffffu, w, k0 + k);
-                                    A.x = fmaf(a[k].x, wk, A.x); A.y = fmaf(a[k].y, wk, A.y);
-                                    A.z = fmaf(a[k].z, wk, A.z); A.w = fmaf(a[k].w, wk, A.w);
-                                }
-#pragma unroll
-                            for (int k = 0; k < kAhead; ++k)
-                                if (k0 + kAhead + k < cnt) a[k] = __ldcg(reinterpret_cast<const float4*>(rh + size_t((p0 + k0 + kAhead + k) * stride)) + lane);
-                        }
+                    for (int d = kQdMergeParts / 2; d; d >>= 1) ls += __shfl_xor_sync(0xffffffffu, ls, d);
+                    L = fmaf(L, keep, __shfl_sync(0xffffffffu, ls, 0));
+                    M = Mn;
+                    A.x *= keep; A.y *= keep; A.z *= keep; A.w *= keep;
+                    cp_async_wait<0>();                   // (a lane reads what it copied)
+#pragma unroll 4
+                    for (int k = 0; k < cnt; ++k) {
+                        const float wk = __shfl_sync(0xffffffffu, w, k);
+                        const float4 a = *reinterpret_cast<const float4*>(to + k * kHeadDim);
+                        A.x = fmaf(a.x, wk, A.x); A.y = fmaf(a.y, wk, A.y);
+                        A.z = fmaf(a.z, wk, A.z); A.w = fmaf(a.w, wk, A.w);
                     }
-                    const float inv = L == 0.f ? 0.f : 1.f / L;
-                    const __nv_bfloat162 o0 = __floats2bfloat162_rn(A.x * inv, A.y * inv), o1 = __floats2bfloat162_rn(A.z * inv, A.w * inv);
-                    __nv_bfloat162* oi = reinterpret_cast<__nv_bfloat162*>(o + hl * kHeadDim + lane * 4);
-                    oi[0] = o0; oi[1] = o1;
                 }
+                const float inv = L == 0.f ? 0.f : 1.f / L;
+                __nv_bfloat162* oi = reinterpret_cast<__nv_bfloat162*>(out + (size_t(done) * n + hl) * kHeadDim + lane * 4);
+                oi[0] = __floats2bfloat162_rn(A.x * inv, A.y * inv);
+                oi[1] = __floats2bfloat162_rn(A.z * inv, A.w * inv);
             }
+            if (t < t_end) { fence_proxy_async_smem(); __syncwarp(); }
         }
     }
     cp_async_wait<0>();
