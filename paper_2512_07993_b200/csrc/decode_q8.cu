@@ -22,7 +22,6 @@
 #include "mma.cuh"
 #include "q8.cuh"
 #include "steer.cuh"
-#include "tc.cuh"
 
 namespace skipkv {
 
@@ -45,14 +44,25 @@ static_assert(kQdThreads == kHeadDim, "a thread merges one channel");
 
 // D[16 x 8] += A[16 x 16] B[16 x 8], f16 operands, fp32 accumulators; the first form has no sum to add to
 __device__ __forceinline__ void mma16816h(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
                  : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
 __device__ __forceinline__ void mma16816h_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
                  : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                  : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
+}
+// D[16 x 8] (+)= A[16 x 32] B[32 x 8], e4m3 operands, fp32 accumulators
+__device__ __forceinline__ void mma16832q(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%0, %1, %2, %3};"
+        : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void mma16832q_first(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0, %1, %2, %3}, {%4, %5, %6, %7}, {%8, %9}, {%10, %10, %10, %10};"
+        : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1), "f"(0.f));
 }
 __device__ __forceinline__ uint32_t pack_f16(float lo, float hi) {
     uint32_t r;
@@ -70,6 +80,13 @@ __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     asm volatile("ld.shared.v4.u32 {%0, %1, %2, %3}, [%4];" : "=r"(r.x), "=r"(r.y), "=r"(r.z), "=r"(r.w) : "r"(addr) : "memory");
     return r;
 }
+// 16 bytes global -> shared, asynchronously (rows are 128 bytes: no more than that is asked of L2); bytes = 0 writes zeros and reads nothing
+__device__ __forceinline__ void cp_async_piece(uint32_t dst, const void* src, int bytes) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ void cp_async_piece(uint32_t dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global.L2::128B [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
+}
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
@@ -77,28 +94,20 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
 // kFew: up to four heads per group (the eight columns are then the heads twice)
 template <int kFmt, bool kFew>
 __global__ void __launch_bounds__(kQdThreads, 2)
-decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constant__ CUtensorMap v_map, int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, const __nv_bfloat16* q, Q8View c,
-                 const int32_t* kv_len, __nv_bfloat16* out, Header* hdr, uint32_t* dec_cnt, float* dec_part, int d_model,
+decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, const __nv_bfloat16* q, Q8View c,
+                 const int32_t* kv_len, __nv_bfloat16* out, uint32_t* status, uint32_t* dec_cnt, float* dec_part, int d_model,
                  __nv_bfloat16* hidden, const __nv_bfloat16* steer_vec, const float* alpha, const uint8_t* flag) {
-    extern __shared__ uint8_t dsm_raw[];
-    uint8_t* const dsm = dsm_raw + ((1024u - (smem_u32(dsm_raw) & 1023u)) & 1023u);      // (the swizzle goes by the address)
+    extern __shared__ __align__(128) uint8_t dsm[];
     const int n = Hq / Hk;                                                   // heads per group
     int* pref = reinterpret_cast<int*>(dsm + kQdRingBytes);                  // [n_slabs + 1] tile prefix
     int* lens = pref + n_slabs + 1;                                          // [n_slabs]
     __shared__ __align__(16) float s_scale[kQdWarps][kQdStages][4];          // of each stage's key rows (two groups of 16), then of its value rows
     __shared__ float2 s_ml[kQdWarps][kMaxGroup];                             // a segment's maxima and sums
     __shared__ uint32_t s_wsum[kQdWarps];
-    __shared__ __align__(8) uint64_t s_full[kQdWarps][kQdStages];            // a stage's copies have landed
-    __shared__ int s_last, s_abort;
+    __shared__ int s_last;
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = gridDim.x, cta = blockIdx.x;
-    if (lane == 0) {
-#pragma unroll
-        for (int i = 0; i < kQdStages; ++i) mbar_init(&s_full[warp][i], 1);
-        mbar_fence_init();
-        if (warp == 0) s_abort = 0;
-    }
     // ---- schedule: CTA k has the tiles [k T / Ge, (k + 1) T / Ge) of the T tiles, Ge = the CTAs that have work.  The lengths may be written by
     // the launch ahead of this one, but the number of tiles they make is mostly older (a step adds one row).  So the schedule is derived from what
     // they are now, the CTA's first tiles are started towards L2 (the point of coherence, so a row that is still being written is not read too
@@ -147,17 +156,17 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             asm volatile("prefetch.global.L2 [%0];" ::"l"(((tid & 1) ? c.v_scale : c.k_scale) + at));
         }
     }
-    if (tid < 2) tmap_prefetch(tid ? &v_map : &k_map);
     pdl_wait();
 
     // ---- copies: this warp's 16 rows of the CTA's k-th tile, and their two scales, go to stage k % kQdStages.  The cursor walks the slab
     // parts of the tile range; divisions and the slab's tables are read once per part, a page's entry a tile ahead.
-    uint8_t* const ring_p = dsm + warp * kQdStages * kQdStageBytes;
-    const uint32_t ring = smem_u32(ring_p), limit = load_wait_limit(hdr);
+    const uint32_t ring = smem_u32(dsm) + warp * kQdStages * kQdStageBytes;
+    const int c_row = lane >> 3, c_col = lane & 7;
+    const uint32_t dst0 = ring + c_row * kQ8RowBytes + ((c_col ^ c_row) << 4);        // row 4 i + c_row, i even; odd: ^ 64
     const float* const sp = (lane & 2) ? c.v_scale : c.k_scale;
     const uint32_t sp_dst = smem_u32(&s_scale[warp][0][lane & 3]);
     const int per_tile = kQ8Tile >> c.block_log2, sub = (warp * kQdRows + (lane & 1) * 16) >> c.block_log2;
-    int p_t = t_begin, p_slab = slab, p_end = t_begin, p_rows = 0, p_stage = 0, fills = 0;
+    int p_t = t_begin, p_slab = slab, p_end = t_begin, p_rows = 0, p_stage = 0;
     int p_row = 0, p_scale = 0, p_page = 0;               // row of this warp's part, place of its scale; paged: the page
     const int32_t* p_table = c.table;
     const int all_scales = c.table ? 0x7fffffff : n_slabs * c.max_blocks;
@@ -193,49 +202,54 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             skip &= ~(1u << p_stage);
             if (rows > 0 && in && p_row < int(c.rows)) {
                 // all 32 rows, also where the slab has fewer left: what follows them is not used (zeros behind the buffer)
-                if (lane == 0) {
-                    uint64_t* const bar = &s_full[warp][p_stage];
-                    uint8_t* const to = ring_p + p_stage * kQdStageBytes;
-                    mbar_expect_tx(bar, kQdStageBytes);
-                    tma_load_2d(to, &k_map, 0, p_row, bar);
-                    tma_load_2d(to + kQdRows * kQ8RowBytes, &v_map, 0, p_row, bar);
+                const size_t off = size_t(uint32_t(p_row + c_row)) * kQ8RowBytes + c_col * 16;
+                const uint8_t *kp = c.K + off, *vp = c.V + off;
+                const uint32_t to = dst0 + p_stage * kQdStageBytes;
+                if (p_row + kQdRows <= int(c.rows)) {
+#pragma unroll
+                    for (int i = 0; i < kQdRows / 4; ++i) {
+                        cp_async_piece((to ^ ((i & 1) << 6)) + i * 4 * kQ8RowBytes, kp + i * 4 * kQ8RowBytes);
+                        cp_async_piece((to ^ ((i & 1) << 6)) + (kQdRows + i * 4) * kQ8RowBytes, vp + i * 4 * kQ8RowBytes);
+                    }
+                } else {
+#pragma unroll 1
+                    for (int i = 0; i < kQdRows / 4; ++i) {
+                        const int bytes = p_row + c_row + 4 * i < int(c.rows) ? 16 : 0;
+                        cp_async_piece((to ^ ((i & 1) << 6)) + i * 4 * kQ8RowBytes, bytes ? kp + i * 4 * kQ8RowBytes : c.K, bytes);
+                        cp_async_piece((to ^ ((i & 1) << 6)) + (kQdRows + i * 4) * kQ8RowBytes, bytes ? vp + i * 4 * kQ8RowBytes : c.V, bytes);
+                    }
                 }
                 if (lane < 4 && ((lane & 1) == 0 || rows > 16)) cp_async4(sp_dst + p_stage * 16, sp + min(p_scale, all_scales - 1));
             } else {
                 skip |= 1u << p_stage;
                 far = far || (early && !in);
-                if (lane == 0) {
-                    mbar_arrive(&s_full[warp][p_stage]);
-                    if (rows > 0 && !early) atomicOr(&hdr->status, SKIPKV_STATUS_BAD_TABLE);
-                }
+                if (lane == 0 && rows > 0 && !early) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
             }
             p_rows -= kQ8Tile;
             p_row = min(p_row + kQ8Tile, int(c.rows));
             p_scale += per_tile;
             ++p_t;
-            ++fills;
             if (++p_stage == kQdStages) p_stage = 0;
         }
-        cp_async_commit();                                // (of the scales; empty groups keep the count)
+        cp_async_commit();                                // empty groups keep the count
     };
-    __syncwarp();
     // What else comes from memory before the first tile is requested here and consumed behind the first copies.
     const int g = lane >> 2, qd = lane & 3;               // mma fragments: rows (tokens, channels) g and g + 8, columns (heads) 2 qd and 2 qd + 1
-    uint32_t qa[8][2];
-    auto fetch_q = [&](int slab_) {                       // a slab's queries: head g (few: g & 3), channels 32 qd to 32 qd + 31
-        const int hd = kFew ? g & 3 : g;
+    // Few heads: columns 2 h and 2 h + 1 belong to head h (high and low parts), so a lane has one head, qd; else column h to head h.
+    const int hd = kFew ? g >> 1 : g;                     // head of this lane's column of the B operands
+    uint32_t qa[16];                                      // bf16 pairs as they come; then the operand
+    auto fetch_q = [&](int slab_) {                       // a slab's queries: channels 32 qd to 32 qd + 31 of head hd
         const uint4* qp = reinterpret_cast<const uint4*>(q + (size_t(slab_) * n + min(hd, n - 1)) * kHeadDim + qd * 32);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const uint4 v = hd < n ? qp[i] : make_uint4(0u, 0u, 0u, 0u);
-            qa[2 * i][0] = v.x; qa[2 * i][1] = v.y; qa[2 * i + 1][0] = v.z; qa[2 * i + 1][1] = v.w;
+            qa[4 * i] = v.x; qa[4 * i + 1] = v.y; qa[4 * i + 2] = v.z; qa[4 * i + 3] = v.w;
         }
     };
     int q_slab = slab;
     if (t_begin < t_end) fetch_q(slab);
     const int len_again = s_lo < s_hi ? length(s_lo) : 0;
     const long long row_again = first_row();
-    int issued = -1, c_stage = 0;                         // issued: copies that were started when a wait gave up
 #pragma unroll 1
     for (int attempt = 0;; ++attempt) {
 #pragma unroll 1
@@ -254,16 +268,12 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             if (p_t < p_end) p_rows = lens[p_slab] - (p_t - pref[p_slab] - kQdPartCost) * kQ8Tile - warp * kQdRows;      // (a length within its last tile)
             break;
         }
-        // another schedule: what is on its way is waited for and left
+        // another schedule: what is on its way is waited for, and its place used anew
         cp_async_wait<0>();
-        for (int k = 0; k < fills && issued < 0; ++k)
-            if (!warp_wait(&s_full[warp][k], 0u, limit, &s_abort, &hdr->status)) issued = fills;
         derive();
         row_first = first_row();
-        p_t = p_end = t_begin; p_slab = slab;
-        c_stage = p_stage;
+        p_t = p_end = t_begin; p_slab = slab; p_stage = 0;
         q_slab = -1;
-        if (issued >= 0) p_t = p_end = t_end;             // (a wait gave up: no more copies)
     }
     pdl_trigger();
 
@@ -275,26 +285,49 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             steer_store(i, vec_per_row, hidden, steer_load(i, vec_per_row, hidden, steer_vec, alpha, flag));
     }
 
-    // The B operand: column g (head), channels 32 qd + 4 ks + {0, 1} and {2, 3} in step ks, times 2^shift; unshift takes the two heads of the
-    // accumulator's columns back.
+    // The B operand of S = K Q^T, times 2^shift; unshift takes the heads of the accumulator's columns back.
+    //  int8 (codes as f16): step i has channels 32 qd + 4 i + {0, 1} in qa[2 i] and {2, 3} in qa[2 i + 1], the largest magnitude in
+    //  [2^14, 2^15); few heads: even columns only.
+    //  e4m3 (codes as they are): the largest magnitude in [2^7, 2^8) and two e4m3 parts, high and 2^5 times the rest, together the 8 bits of
+    //  every bf16 from 2^-15 of the head's largest on (a smaller one is rounded to 2^-23 of that).  Step i has channels 32 qd + 8 i + {0 to 3} in
+    //  qa[2 i] and {4 to 7} in qa[2 i + 1]; low parts in odd columns (few heads) or in q_lo.
     float2 unshift = make_float2(1.f, 1.f);
+    uint32_t q_lo[8];
     auto shift_q = [&]() {
         uint32_t m = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) m = __vmaxu2(m, __vmaxu2(qa[i][0] & 0x7fff7fffu, qa[i][1] & 0x7fff7fffu));
+        for (int i = 0; i < 16; ++i) m = __vmaxu2(m, qa[i] & 0x7fff7fffu);
         m = max(m & 0xffffu, m >> 16);
         m = max(m, __shfl_xor_sync(0xffffffffu, m, 1));
         m = max(m, __shfl_xor_sync(0xffffffffu, m, 2));
-        const int field = min(max(268 - int(m >> 7), 1), 253);     // of 2^shift: the largest magnitude goes to [2^14, 2^15)
+        const int field = min(max((kFmt == SKIPKV_Q8_E4M3 ? 261 : 268) - int(m >> 7), 1), 253);       // exponent field of 2^shift
         const float up = __uint_as_float(uint32_t(field) << 23);
+        if (kFmt == SKIPKV_Q8_E4M3) {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-#pragma unroll
-            for (int k = 0; k < 2; ++k) {
-                const float2 v = bf16x2_to_f2(qa[i][k]);
-                qa[i][k] = pack_f16(v.x * up, v.y * up);
+            for (int i = 0; i < 8; ++i) {
+                const float2 v0 = bf16x2_to_f2(qa[2 * i]), v1 = bf16x2_to_f2(qa[2 * i + 1]);
+                const float y[4] = {v0.x * up, v0.y * up, v1.x * up, v1.y * up};
+                const uint32_t hi = q8_round<SKIPKV_Q8_E4M3>(y[0], y[1], y[2], y[3]);
+                uint32_t h0, h1;
+                q8_to_f16<SKIPKV_Q8_E4M3>(hi, h0, h1);
+                const float2 f0 = f16x2_to_f2(h0), f1 = f16x2_to_f2(h1);
+                const uint32_t lo = q8_round<SKIPKV_Q8_E4M3>((y[0] - f0.x) * 32.f, (y[1] - f0.y) * 32.f, (y[2] - f1.x) * 32.f, (y[3] - f1.y) * 32.f);
+                if (kFew) {
+                    qa[i] = (g & 1) ? lo : hi;
+                } else {
+                    qa[i] = hi;                           // (qa[2 i] and qa[2 i + 1] have been read)
+                    q_lo[i] = lo;
+                }
             }
-        const float down = __uint_as_float(uint32_t(254 - field) << 23);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                const float2 v = bf16x2_to_f2(qa[i]);
+                qa[i] = kFew && (g & 1) ? 0u : pack_f16(v.x * up, v.y * up);
+            }
+        }
+        // (an infinity or a NaN in a head makes its logits NaN, as its products would)
+        const float down = __uint_as_float(m < 0x7f80u ? uint32_t(254 - field) << 23 : 0x7fffffffu);
         unshift = make_float2(__shfl_sync(0xffffffffu, down, 8 * qd), __shfl_sync(0xffffffffu, down, 8 * qd + 4));
     };
 
@@ -304,10 +337,10 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
     const uint32_t v_at = ring + (kQdRows + 2 * qd) * kQ8RowBytes + ((g ^ (2 * qd)) << 4);
     const uint32_t v_at1 = (v_at ^ 16u) + kQ8RowBytes;
 
+    int c_stage = 0;
     // a warp's sums of a segment lie in the stage of its last tile
     auto sums = [&](int w) { return reinterpret_cast<float*>(dsm + (size_t(w) * kQdStages + (c_stage == 0 ? kQdStages - 1 : c_stage - 1)) * kQdStageBytes); };
     int t = t_begin;
-    uint32_t parity = 0;                                  // (of the stage's copies: a discarded first round moves on the stage, never past the last)
     // The slab whose part this CTA has delivered, and the answer to its arrival, which nothing waits for before the next part is worked on.
     int pend = -1, pend_parts = 0, pend_cta = 0;
     uint32_t pend_old = 0;
@@ -325,7 +358,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
         if (slab != q_slab) { fetch_q(slab); q_slab = slab; }
         shift_q();
         q_slab = -1;
-        float2 acc[8][2];                                 // channels 16 g + 2 j and 16 g + 2 j + 1 of the lane's two heads
+        float2 acc[8][2];                                 // channels 16 g + 2 j and 16 g + 2 j + 1 of the lane's two columns
 #pragma unroll
         for (int j = 0; j < 8; ++j) acc[j][0] = acc[j][1] = make_float2(0.f, 0.f);
         float2 m = make_float2(-INFINITY, -INFINITY), l = make_float2(0.f, 0.f);    // their running maximum, this lane's share of the sum
@@ -333,15 +366,14 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
 #pragma unroll 1
         for (; t < seg_end; ++t, rows_left -= kQ8Tile) {
             cp_async_wait<kQdStages - 2>();
-            const bool landed = warp_wait(&s_full[warp][c_stage], parity, limit, &s_abort, &hdr->status);
-            if (!landed && issued < 0) issued = fills;        // from here on this warp copies nothing and works on nothing
-            const bool live = issued < 0 && rows_left > 0 && !((skip >> c_stage) & 1u);
-            if (issued < 0) issue_next(false);
+            __syncwarp();                                 // every lane's pieces have landed; the stage before is read out
+            const bool live = rows_left > 0 && !((skip >> c_stage) & 1u);
+            issue_next(false);
             if (live) {
                 const uint32_t so = c_stage * kQdStageBytes;
                 const float4 scales = *reinterpret_cast<const float4*>(s_scale[warp][c_stage]);
                 const bool two = rows_left > 16;          // the second group has rows
-                float s[2][2][4];                         // per group two chains of four steps each
+                float s[2][2][4];                         // per group: two chains (int8), high and low parts (e4m3, many heads), one (few)
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
 #pragma unroll
@@ -349,13 +381,26 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                         const uint32_t at = ((k_at + so) ^ (half << 4)) + u * 16 * kQ8RowBytes;
                         const uint4 k0 = lds128(at), k1 = lds128(at + 8 * kQ8RowBytes);
                         const uint32_t lo[4] = {k0.x, k0.y, k0.z, k0.w}, hi[4] = {k1.x, k1.y, k1.z, k1.w};
+                        if (kFmt == SKIPKV_Q8_E4M3) {
 #pragma unroll
-                        for (int i = 0; i < 4; ++i) {
-                            uint32_t a0, a1, a2, a3;
-                            q8_to_f16<kFmt>(lo[i], a0, a2);
-                            q8_to_f16<kFmt>(hi[i], a1, a3);
-                            if (half == 0 && i < 2) mma16816h_first(s[u][i & 1], a0, a1, a2, a3, qa[4 * half + i][0], qa[4 * half + i][1]);
-                            else                    mma16816h(s[u][i & 1], a0, a1, a2, a3, qa[4 * half + i][0], qa[4 * half + i][1]);
+                            for (int i = 0; i < 2; ++i) {
+                                const int k = 2 * half + i;
+                                if (k == 0) mma16832q_first(s[u][0], lo[0], hi[0], lo[1], hi[1], qa[0], qa[1]);
+                                else        mma16832q(s[u][0], lo[2 * i], hi[2 * i], lo[2 * i + 1], hi[2 * i + 1], qa[2 * k], qa[2 * k + 1]);
+                                if (kFew) continue;
+                                if (k == 0) mma16832q_first(s[u][1], lo[0], hi[0], lo[1], hi[1], q_lo[0], q_lo[1]);
+                                else        mma16832q(s[u][1], lo[2 * i], hi[2 * i], lo[2 * i + 1], hi[2 * i + 1], q_lo[2 * k], q_lo[2 * k + 1]);
+                            }
+                        } else {
+#pragma unroll
+                            for (int i = 0; i < 4; ++i) {
+                                uint32_t a0, a1, a2, a3;
+                                q8_to_f16<kFmt>(lo[i], a0, a2);
+                                q8_to_f16<kFmt>(hi[i], a1, a3);
+                                const int k = 4 * half + i;
+                                if (k < 2) mma16816h_first(s[u][i & 1], a0, a1, a2, a3, qa[2 * k], qa[2 * k + 1]);
+                                else       mma16816h(s[u][i & 1], a0, a1, a2, a3, qa[2 * k], qa[2 * k + 1]);
+                            }
                         }
                     }
                 uint4 v[2][4];                            // value rows 2 qd, 2 qd + 1, 2 qd + 8, 2 qd + 9 of each group
@@ -364,61 +409,99 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     v[u][0] = lds128(v_at + so + u * 16 * kQ8RowBytes); v[u][1] = lds128(v_at1 + so + u * 16 * kQ8RowBytes);
                     v[u][2] = lds128(v_at + so + (u * 16 + 8) * kQ8RowBytes); v[u][3] = lds128(v_at1 + so + (u * 16 + 8) * kQ8RowBytes);
                 }
-                // this lane's logits: tokens g and g + 8 of either group, its two heads (packed fp32 arithmetic: a pair of heads per instruction)
-                float2 x[2], y[2];
-#pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    const float f = qscale * (u ? scales.y : scales.x);
-                    const float2 f2 = make_float2(f * unshift.x, f * unshift.y);
-                    x[u] = __fmul2_rn(__fadd2_rn(make_float2(s[u][0][0], s[u][0][1]), make_float2(s[u][1][0], s[u][1][1])), f2);
-                    y[u] = __fmul2_rn(__fadd2_rn(make_float2(s[u][0][2], s[u][0][3]), make_float2(s[u][1][2], s[u][1][3])), f2);
-                }
-                if (rows_left < kQdRows) {                // the end of the slab: rows behind it hold anything, NaN too
+                uint32_t ph[2][2], pl[2][2];              // P^T as B operands: (few) high parts in even and low ones in odd columns, else apart
+                if (kFew) {
+                    // this lane's logits: tokens g and g + 8 of either group, head qd
+                    float x[2][2];
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const int left = rows_left - 16 * u;
-                        if (g >= left) x[u] = make_float2(-INFINITY, -INFINITY);
-                        if (g + 8 >= left) y[u] = make_float2(-INFINITY, -INFINITY);
+                        const float f = qscale * (u ? scales.y : scales.x) * unshift.x;
 #pragma unroll
-                        for (int k = 0; k < 4; ++k)
-                            if (2 * qd + (k & 1) + (k >> 1) * 8 >= left) v[u][k] = make_uint4(0u, 0u, 0u, 0u);
+                        for (int r = 0; r < 2; ++r)
+                            x[u][r] = f * (kFmt == SKIPKV_Q8_E4M3 ? fmaf(s[u][0][2 * r + 1], 0.03125f, s[u][0][2 * r]) : s[u][0][2 * r] + s[u][1][2 * r]);
                     }
-                }
-                float2 top = make_float2(fmaxf(fmaxf(x[0].x, y[0].x), fmaxf(x[1].x, y[1].x)), fmaxf(fmaxf(x[0].y, y[0].y), fmaxf(x[1].y, y[1].y)));
-                if (__any_sync(0xffffffffu, top.x > m.x || top.y > m.y)) {
+                    if (rows_left < kQdRows) {            // the end of the slab: rows behind it hold anything, NaN too
 #pragma unroll
-                    for (int d = 4; d < 32; d <<= 1) {
-                        top.x = fmaxf(top.x, __shfl_xor_sync(0xffffffffu, top.x, d));
-                        top.y = fmaxf(top.y, __shfl_xor_sync(0xffffffffu, top.y, d));
+                        for (int u = 0; u < 2; ++u)
+#pragma unroll
+                            for (int r = 0; r < 2; ++r)
+                                if (16 * u + 8 * r + g >= rows_left) x[u][r] = -INFINITY;
                     }
-                    top = make_float2(fmaxf(top.x, m.x), fmaxf(top.y, m.y));
-                    const float2 sc = make_float2(ex2(m.x - top.x), ex2(m.y - top.y));   // first rows: 2^(-inf) = 0
-                    l = __fmul2_rn(l, sc);
+                    float top = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
+                    if (__any_sync(0xffffffffu, top > m.x)) {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j) { acc[j][0] = __fmul2_rn(acc[j][0], sc); acc[j][1] = __fmul2_rn(acc[j][1], sc); }
-                    m = top;
-                }
-                // 2^15 p
-                const float2 neg = make_float2(15.f - m.x, 15.f - m.y);
+                        for (int d = 4; d < 32; d <<= 1) top = fmaxf(top, __shfl_xor_sync(0xffffffffu, top, d));
+                        top = fmaxf(top, m.x);
+                        const float sc = ex2(m.x - top);  // first rows: 2^(-inf) = 0
+                        l.x *= sc;
+                        m.x = top;
+                        const float2 sc2 = make_float2(sc, sc);
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    x[u] = __fadd2_rn(x[u], neg); y[u] = __fadd2_rn(y[u], neg);
-                    x[u] = make_float2(ex2(x[u].x), ex2(x[u].y)); y[u] = make_float2(ex2(y[u].x), ex2(y[u].y));
-                }
-                l = __fadd2_rn(l, __fadd2_rn(__fadd2_rn(x[0], y[0]), __fadd2_rn(x[1], y[1])));
-                uint32_t ph[2][2], pl[2][2];
+                        for (int j = 0; j < 8; ++j) { acc[j][0] = __fmul2_rn(acc[j][0], sc2); acc[j][1] = __fmul2_rn(acc[j][1], sc2); }
+                    }
+                    const float neg = 15.f - m.x;         // 2^15 p
 #pragma unroll
-                for (int u = 0; u < 2; ++u) {
-                    uint32_t hx, lx, hy, ly;
-                    split_f16(x[u], hx, lx);
-                    split_f16(y[u], hy, ly);
-                    if (kFew) {
-                        const bool first = qd < 2;        // this lane's columns hold high parts (the others low ones)
-                        ph[u][0] = movmatrix_trans(first ? hx : lx); ph[u][1] = movmatrix_trans(first ? hy : ly);
-                    } else {
+                    for (int u = 0; u < 2; ++u) {
+#pragma unroll
+                        for (int r = 0; r < 2; ++r) x[u][r] = ex2(x[u][r] + neg);
+                        const float2 hi = f16x2_to_f2(pack_f16(x[u][0], x[u][1]));
+                        ph[u][0] = movmatrix_trans(pack_f16(x[u][0], x[u][0] - hi.x));
+                        ph[u][1] = movmatrix_trans(pack_f16(x[u][1], x[u][1] - hi.y));
+                    }
+                    l.x += (x[0][0] + x[0][1]) + (x[1][0] + x[1][1]);
+                } else {
+                    // the same for heads 2 qd and 2 qd + 1 (packed fp32 arithmetic: the two heads per instruction)
+                    float2 x[2], y[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const float f = qscale * (u ? scales.y : scales.x);
+                        const float2 f2 = make_float2(f * unshift.x, f * unshift.y);
+                        const float2 a = make_float2(s[u][0][0], s[u][0][1]), b = make_float2(s[u][0][2], s[u][0][3]);
+                        const float2 a1 = make_float2(s[u][1][0], s[u][1][1]), b1 = make_float2(s[u][1][2], s[u][1][3]);
+                        const float part = kFmt == SKIPKV_Q8_E4M3 ? 0.03125f : 1.f;
+                        x[u] = __fmul2_rn(__ffma2_rn(a1, make_float2(part, part), a), f2);
+                        y[u] = __fmul2_rn(__ffma2_rn(b1, make_float2(part, part), b), f2);
+                    }
+                    if (rows_left < kQdRows) {
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            if (16 * u + g >= rows_left) x[u] = make_float2(-INFINITY, -INFINITY);
+                            if (16 * u + 8 + g >= rows_left) y[u] = make_float2(-INFINITY, -INFINITY);
+                        }
+                    }
+                    float2 top = make_float2(fmaxf(fmaxf(x[0].x, y[0].x), fmaxf(x[1].x, y[1].x)), fmaxf(fmaxf(x[0].y, y[0].y), fmaxf(x[1].y, y[1].y)));
+                    if (__any_sync(0xffffffffu, top.x > m.x || top.y > m.y)) {
+#pragma unroll
+                        for (int d = 4; d < 32; d <<= 1) {
+                            top.x = fmaxf(top.x, __shfl_xor_sync(0xffffffffu, top.x, d));
+                            top.y = fmaxf(top.y, __shfl_xor_sync(0xffffffffu, top.y, d));
+                        }
+                        top = make_float2(fmaxf(top.x, m.x), fmaxf(top.y, m.y));
+                        const float2 sc = make_float2(ex2(m.x - top.x), ex2(m.y - top.y));
+                        l = __fmul2_rn(l, sc);
+#pragma unroll
+                        for (int j = 0; j < 8; ++j) { acc[j][0] = __fmul2_rn(acc[j][0], sc); acc[j][1] = __fmul2_rn(acc[j][1], sc); }
+                        m = top;
+                    }
+                    const float2 neg = make_float2(15.f - m.x, 15.f - m.y);
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        x[u] = __fadd2_rn(x[u], neg); y[u] = __fadd2_rn(y[u], neg);
+                        x[u] = make_float2(ex2(x[u].x), ex2(x[u].y)); y[u] = make_float2(ex2(y[u].x), ex2(y[u].y));
+                        uint32_t hx, lx, hy, ly;
+                        split_f16(x[u], hx, lx);
+                        split_f16(y[u], hy, ly);
                         ph[u][0] = movmatrix_trans(hx); ph[u][1] = movmatrix_trans(hy);
                         pl[u][0] = movmatrix_trans(lx); pl[u][1] = movmatrix_trans(ly);
                     }
+                    l = __fadd2_rn(l, __fadd2_rn(__fadd2_rn(x[0], y[0]), __fadd2_rn(x[1], y[1])));
+                }
+                if (rows_left < kQdRows) {
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int k = 0; k < 4; ++k)
+                            if (16 * u + 2 * qd + (k & 1) + (k >> 1) * 8 >= rows_left) v[u][k] = make_uint4(0u, 0u, 0u, 0u);
                 }
                 const float2 vs2[2] = {make_float2(scales.z, scales.z), two ? make_float2(scales.w, scales.w) : make_float2(0.f, 0.f)};
 #pragma unroll
@@ -442,8 +525,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     }
                 }
             }
-            __syncwarp();                                 // the stage is read out: the next copies may go there
-            if (++c_stage == kQdStages) { c_stage = 0; parity ^= 1u; }
+            if (++c_stage == kQdStages) c_stage = 0;
         }
 
         // -------------------------------------------------------------- the end of a segment
@@ -452,9 +534,16 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             l.x += __shfl_xor_sync(0xffffffffu, l.x, d);
             l.y += __shfl_xor_sync(0xffffffffu, l.y, d);
         }
-        // The columns' sums (few: high and low parts apart) go to the stage of the tile that was worked on last: its rows are read out, and the
-        // next copy into it is issued behind the barriers below.
-        {
+        // The heads' sums go to the stage of the tile that was worked on last: its rows are read out, and the next copy into it is issued behind
+        // the barriers below.
+        if (kFew) {
+            float4* wp = reinterpret_cast<float4*>(sums(warp) + size_t(qd) * kQdSumStride + 16 * g);
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                wp[j] = make_float4(acc[2 * j][0].x + acc[2 * j][0].y, acc[2 * j][1].x + acc[2 * j][1].y, acc[2 * j + 1][0].x + acc[2 * j + 1][0].y,
+                                    acc[2 * j + 1][1].x + acc[2 * j + 1][1].y);
+            if (g == 0) s_ml[warp][qd] = make_float2(m.x, l.x);
+        } else {
             float* wp = sums(warp) + size_t(2 * qd) * kQdSumStride + 16 * g;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -463,7 +552,6 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
             }
             if (g == 0) { s_ml[warp][2 * qd] = make_float2(m.x, l.x); s_ml[warp][2 * qd + 1] = make_float2(m.y, l.y); }
         }
-        if (t < t_end) fence_proxy_async_smem();          // (the stage's next writer is a bulk copy)
         }
         if (pend >= 0 && tid == 0) {
             const int last = pend_old == uint32_t(pend_parts - 1) ? 1 : 0;
@@ -487,9 +575,8 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 for (int w = 0; w < kQdWarps; ++w) {
                     const float2 ml = s_ml[w][hl];
                     const float e = ex2(ml.x - M);
-                    const float* p = sums(w) + hl * kQdSumStride + tid;
                     L = fmaf(ml.y, e, L);
-                    A = fmaf(kFew ? p[0] + p[4 * kQdSumStride] : p[0], e, A);
+                    A = fmaf(sums(w)[hl * kQdSumStride + tid], e, A);
                 }
                 if (n_part == 1) {
                     o[hl * kHeadDim + tid] = __float2bfloat16_rn(L == 0.f ? 0.f : A / L);
@@ -523,7 +610,7 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                     const bool on = lane < cnt;
                     const float2 ml = __ldcg(reinterpret_cast<const float2*>(rh + size_t(p0 + min(lane, cnt - 1)) * stride + kHeadDim));
 #pragma unroll 4
-                    for (int k = 0; k < cnt; ++k) cp_async16(smem_u32(to + k * kHeadDim), rh + size_t(p0 + k) * stride + lane * 4);
+                    for (int k = 0; k < cnt; ++k) cp_async_piece(smem_u32(to + k * kHeadDim), rh + size_t(p0 + k) * stride + lane * 4);
                     cp_async_commit();
                     float mx = on ? ml.x : -INFINITY;
 #pragma unroll
@@ -551,14 +638,9 @@ decode_q8_kernel(const __grid_constant__ CUtensorMap k_map, const __grid_constan
                 oi[0] = __floats2bfloat162_rn(A.x * inv, A.y * inv);
                 oi[1] = __floats2bfloat162_rn(A.z * inv, A.w * inv);
             }
-            if (t < t_end) { fence_proxy_async_smem(); __syncwarp(); }
         }
     }
     cp_async_wait<0>();
-    // (every copy has been waited for; where a wait gave up, those in flight are waited for here)
-#pragma unroll 1
-    for (int k = max(issued - kQdStages, 0); k < issued; ++k)
-        (void)mbar_wait(&s_full[warp][k % kQdStages], uint32_t(k / kQdStages) & 1u, kRetirePolls);
     // slabs with no row to attend to: zeros (owned round-robin)
 #pragma unroll 1
     for (int s = cta; s < n_slabs; s += G) {
@@ -590,17 +672,14 @@ extern "C" int skipkv_decode_attn_q8(const skipkv_shape* shape, const skipkv_q8_
     }
     if (!cache->block_table && int64_t(L.slabs) * cache->max_blocks > 0x7fffffff) return SKIPKV_ERR_UNSUPPORTED;      // places of scales in 32 bits
     uint8_t* w = static_cast<uint8_t*>(ws);
-    const size_t smem = 1024 + size_t(kQdRingBytes) + size_t(2 * L.slabs + 1) * 4;
-    CUtensorMap km, vm;
-    if (int rc = tmap_codes(&km, cache->K, uint64_t(cache->rows), kQdRows)) return rc;
-    if (int rc = tmap_codes(&vm, cache->V, uint64_t(cache->rows), kQdRows)) return rc;
+    const size_t smem = size_t(kQdRingBytes) + size_t(2 * L.slabs + 1) * 4;
     const int grid = 2 * num_sms() < kQdMaxGrid ? 2 * num_sms() : kQdMaxGrid;
     const auto kernel = cache->format == SKIPKV_Q8_E4M3 ? (L.group <= 4 ? decode_q8_kernel<SKIPKV_Q8_E4M3, true> : decode_q8_kernel<SKIPKV_Q8_E4M3, false>)
                                                         : (L.group <= 4 ? decode_q8_kernel<SKIPKV_Q8_INT8, true> : decode_q8_kernel<SKIPKV_Q8_INT8, false>);
-    SKIPKV_CUDA(launch_dependent(kernel, dim3(grid), dim3(kQdThreads), smem, static_cast<cudaStream_t>(stream), km, vm, int(shape->batch),
+    SKIPKV_CUDA(launch_dependent(kernel, dim3(grid), dim3(kQdThreads), smem, static_cast<cudaStream_t>(stream), int(shape->batch),
                                  int(shape->n_q_heads), int(shape->n_kv_heads), int(L.slabs), shape->slab_off, shape->cap,
                                  static_cast<const __nv_bfloat16*>(q), q8_view(*cache), kv_len, static_cast<__nv_bfloat16*>(out),
-                                 reinterpret_cast<Header*>(w + L.header), reinterpret_cast<uint32_t*>(w + L.dec_cnt),
+                                 &reinterpret_cast<Header*>(w + L.header)->status, reinterpret_cast<uint32_t*>(w + L.dec_cnt),
                                  reinterpret_cast<float*>(w + L.dec_part), int(shape->d_model), static_cast<__nv_bfloat16*>(hidden),
                                  static_cast<const __nv_bfloat16*>(steer_vec), alpha, flag));
     return SKIPKV_OK;
