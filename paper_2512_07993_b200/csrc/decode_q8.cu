@@ -166,68 +166,96 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     const float* const sp = (lane & 2) ? c.v_scale : c.k_scale;
     const uint32_t sp_dst = smem_u32(&s_scale[warp][0][lane & 3]);
     const int per_tile = kQ8Tile >> c.block_log2, sub = (warp * kQdRows + (lane & 1) * 16) >> c.block_log2;
-    int p_t = t_begin, p_slab = slab, p_end = t_begin, p_rows = 0, p_stage = 0;
-    int p_row = 0, p_scale = 0, p_page = 0;               // row of this warp's part, place of its scale; paged: the page
+    int p_t = t_begin, p_slab = slab, p_end = t_begin, p_stage = 0;
+    int p_fast = 0;                                       // tiles ahead that are whole and, contiguous, inside the buffers
+    int p_row0 = 0, p_page = 0;                           // contiguous: row of the slab's first token; paged: page of the next tile
+    size_t p_off = 0;                                     // contiguous: where this lane's pieces of the next tile begin
+    const float* p_sp = nullptr;                          // and the tile's scale
     const int32_t* p_table = c.table;
+    const int pages = int(c.rows / kQ8Tile);
+    const size_t lane_off = size_t(warp * kQdRows + c_row) * kQ8RowBytes + c_col * 16;
     const int all_scales = c.table ? 0x7fffffff : n_slabs * c.max_blocks;
     uint32_t skip = 0;                                    // stages without copies: no rows, or rows that lie outside the buffers
     bool far = false;                                     // a copy was left out under the schedule from before the wait
-    // early: under that schedule, with a length that may be old: all of the tile is copied
+    auto copy_rows = [&](size_t off, const float* scale) {
+        const uint8_t *kp = c.K + off, *vp = c.V + off;
+        const uint32_t to = dst0 + p_stage * kQdStageBytes;
+#pragma unroll
+        for (int i = 0; i < kQdRows / 4; ++i) {
+            cp_async_piece((to ^ ((i & 1) << 6)) + i * 4 * kQ8RowBytes, kp + i * 4 * kQ8RowBytes);
+            cp_async_piece((to ^ ((i & 1) << 6)) + (kQdRows + i * 4) * kQ8RowBytes, vp + i * 4 * kQ8RowBytes);
+        }
+        if (lane < 4) cp_async4(sp_dst + p_stage * 16, scale);
+    };
+    // early: under the schedule from before the wait, with a length that may be old: all of the tile is copied
     auto issue_next = [&](bool early) {
-        if (p_t < t_end) {
+        bool fast = p_fast > 0;
+        if (c.table && uint32_t(p_page) >= uint32_t(pages)) fast = false;
+        if (fast) {
+            if (c.table) {
+                copy_rows(size_t(p_page) * (kQ8Tile * kQ8RowBytes) + lane_off, sp + p_page * per_tile + sub);
+                if (p_t + 1 < p_end) p_page = __ldcg(++p_table);
+            } else {
+                copy_rows(p_off, p_sp);
+                p_off += kQ8Tile * kQ8RowBytes;
+                p_sp += per_tile;
+            }
+            skip &= ~(1u << p_stage);
+            --p_fast;
+            ++p_t;
+            if (++p_stage == kQdStages) p_stage = 0;
+        } else if (p_t < t_end) {
             if (p_t == p_end) {
                 while (pref[p_slab + 1] <= p_t) ++p_slab;
                 p_end = pref[p_slab + 1];
                 p_t = max(p_t, pref[p_slab] + kQdPartCost);
                 if (p_t >= t_end) { p_t = p_end = t_end; cp_async_commit(); return; }
                 const int j = p_t - pref[p_slab] - kQdPartCost;
-                p_rows = lens[p_slab] - j * kQ8Tile - warp * kQdRows;
                 if (c.table) {
                     p_table = c.table + size_t(p_slab) * c.max_pages + j;
                     p_page = p_t == t_begin ? int(row_first) : __ldcg(p_table);
                 } else {
                     const long long row0 = p_t == t_begin ? row_first : (long long)slab_row0(slab_off, cap, Hk, p_slab / Hk, p_slab % Hk);
-                    p_row = int(row0 < 0 ? c.rows : min(row0 + (long long)j * kQ8Tile + warp * kQdRows, c.rows));
-                    p_scale = p_slab * c.max_blocks + j * per_tile + sub;
+                    p_row0 = int(row0 < 0 || row0 > c.rows ? c.rows : row0);
                 }
             }
-            if (c.table) {                                // (a page outside the pool: a row at which nothing lies)
-                const bool in = uint32_t(p_page) < uint32_t(c.rows / kQ8Tile);
-                p_row = in ? p_page * kQ8Tile + warp * kQdRows : int(c.rows);
-                p_scale = in ? p_page * per_tile + sub : 0;
-                if (p_t + 1 < p_end) p_page = __ldcg(++p_table);
-            }
+            const int j = p_t - pref[p_slab] - kQdPartCost, left = lens[p_slab] - j * kQ8Tile, p_rows = left - warp * kQdRows;
+            // (a page outside the pool: a row at which nothing lies; this warp's first row, at most the buffer's end)
+            const int row = c.table ? (uint32_t(p_page) < uint32_t(pages) ? p_page * kQ8Tile + warp * kQdRows : int(c.rows))
+                                    : int(min((long long)p_row0 + (long long)j * kQ8Tile + warp * kQdRows, c.rows));
+            const int place = c.table ? (uint32_t(p_page) < uint32_t(pages) ? p_page * per_tile + sub : 0) : p_slab * c.max_blocks + j * per_tile + sub;
+            if (c.table && p_t + 1 < p_end) p_page = __ldcg(++p_table);
             const int rows = early ? kQdRows : min(p_rows, kQdRows);
-            const bool in = p_row + min(p_rows, kQdRows) <= int(c.rows);
+            const bool in = row + min(p_rows, kQdRows) <= int(c.rows);
             skip &= ~(1u << p_stage);
-            if (rows > 0 && in && p_row < int(c.rows)) {
+            if (rows > 0 && in && row < int(c.rows)) {
                 // all 32 rows, also where the slab has fewer left: what follows them is not used (zeros behind the buffer)
-                const size_t off = size_t(uint32_t(p_row + c_row)) * kQ8RowBytes + c_col * 16;
-                const uint8_t *kp = c.K + off, *vp = c.V + off;
-                const uint32_t to = dst0 + p_stage * kQdStageBytes;
-                if (p_row + kQdRows <= int(c.rows)) {
-#pragma unroll
-                    for (int i = 0; i < kQdRows / 4; ++i) {
-                        cp_async_piece((to ^ ((i & 1) << 6)) + i * 4 * kQ8RowBytes, kp + i * 4 * kQ8RowBytes);
-                        cp_async_piece((to ^ ((i & 1) << 6)) + (kQdRows + i * 4) * kQ8RowBytes, vp + i * 4 * kQ8RowBytes);
-                    }
+                const size_t off = size_t(uint32_t(row + c_row)) * kQ8RowBytes + c_col * 16;
+                const float* scale = sp + min(place, all_scales - 1);
+                if (row + kQdRows <= int(c.rows)) {
+                    copy_rows(off, scale);
                 } else {
+                    const uint32_t to = dst0 + p_stage * kQdStageBytes;
 #pragma unroll 1
                     for (int i = 0; i < kQdRows / 4; ++i) {
-                        const int bytes = p_row + c_row + 4 * i < int(c.rows) ? 16 : 0;
-                        cp_async_piece((to ^ ((i & 1) << 6)) + i * 4 * kQ8RowBytes, bytes ? kp + i * 4 * kQ8RowBytes : c.K, bytes);
-                        cp_async_piece((to ^ ((i & 1) << 6)) + (kQdRows + i * 4) * kQ8RowBytes, bytes ? vp + i * 4 * kQ8RowBytes : c.V, bytes);
+                        const int bytes = row + c_row + 4 * i < int(c.rows) ? 16 : 0;
+                        cp_async_piece((to ^ ((i & 1) << 6)) + i * 4 * kQ8RowBytes, bytes ? c.K + off + i * 4 * kQ8RowBytes : c.K, bytes);
+                        cp_async_piece((to ^ ((i & 1) << 6)) + (kQdRows + i * 4) * kQ8RowBytes, bytes ? c.V + off + i * 4 * kQ8RowBytes : c.V, bytes);
                     }
+                    if (lane < 4) cp_async4(sp_dst + p_stage * 16, scale);
                 }
-                if (lane < 4 && ((lane & 1) == 0 || rows > 16)) cp_async4(sp_dst + p_stage * 16, sp + min(p_scale, all_scales - 1));
             } else {
                 skip |= 1u << p_stage;
                 far = far || (early && !in);
                 if (lane == 0 && rows > 0 && !early) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
             }
-            p_rows -= kQ8Tile;
-            p_row = min(p_row + kQ8Tile, int(c.rows));
-            p_scale += per_tile;
+            // the whole tiles behind it
+            const int whole = lens[p_slab] / kQ8Tile;
+            p_fast = !c.table && (long long)p_row0 + (long long)whole * kQ8Tile > c.rows ? 0 : min(min(p_end, t_end) - p_t, whole - j) - 1;
+            if (!c.table) {
+                p_off = size_t(uint32_t(p_row0)) * kQ8RowBytes + size_t(j + 1) * (kQ8Tile * kQ8RowBytes) + lane_off;
+                p_sp = sp + place + per_tile;
+            }
             ++p_t;
             if (++p_stage == kQdStages) p_stage = 0;
         }
@@ -264,15 +292,12 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             if (tiles(now) != tiles(lens[s]) || (!c.table && (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk) + now > c.rows)) changed = 1;
             lens[s] = now;
         }
-        if (!__syncthreads_or(changed)) {
-            if (p_t < p_end) p_rows = lens[p_slab] - (p_t - pref[p_slab] - kQdPartCost) * kQ8Tile - warp * kQdRows;      // (a length within its last tile)
-            break;
-        }
+        if (!__syncthreads_or(changed)) break;
         // another schedule: what is on its way is waited for, and its place used anew
         cp_async_wait<0>();
         derive();
         row_first = first_row();
-        p_t = p_end = t_begin; p_slab = slab; p_stage = 0;
+        p_t = p_end = t_begin; p_slab = slab; p_stage = p_fast = 0;
         q_slab = -1;
     }
     pdl_trigger();
