@@ -537,7 +537,7 @@ int skipkv_page_tables(int32_t batch, int32_t n_kv_heads, int32_t max_pages, int
 /*
  * skipkv_slot_map -- the pool row of every new token: slots[i][h] = block_table[b][h][t / SKIPKV_PAGE_ROWS] * SKIPKV_PAGE_ROWS +
  * t % SKIPKV_PAGE_ROWS with t = start[b][h] + i - new_off[b], for new_off[b] <= i < new_off[b + 1]; -1 where the slab holds no
- * page for t (t / SKIPKV_PAGE_ROWS >= n_pages[b][h]).  An index for the caller's own copies into the pool.  start, n_pages: device
+ * page for t (t / SKIPKV_PAGE_ROWS >= n_pages[b][h], or a negative entry).  An index for the caller's own copies into the pool.  start, n_pages: device
  * int32 [batch][Hk].  new_off: device int32 [batch + 1], ascending, or NULL: token i belongs to sequence i.  slots: device int64
  * [n_new][Hk]; entries of tokens that belong to no sequence are not written.  n_new = 0 does nothing.
  */

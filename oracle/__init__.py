@@ -402,7 +402,8 @@ def slot_map(table, n_pages, start, new_off, n_kv_heads, n_new, fill, page_rows=
             for h in range(n_kv_heads):
                 s = b * n_kv_heads + h
                 t = int(start[s]) + i - int(new_off[b])
-                out[i, h] = int(table[s][t // page_rows]) * page_rows + t % page_rows if t // page_rows < n_pages[s] else -1
+                page = int(table[s][t // page_rows]) if t // page_rows < n_pages[s] else -1
+                out[i, h] = page * page_rows + t % page_rows if page >= 0 else -1
     return out
 
 

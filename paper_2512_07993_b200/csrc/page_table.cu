@@ -16,6 +16,7 @@ namespace skipkv {
 constexpr int kPtThreads = 256;
 constexpr int kPtWarps = kPtThreads / 32;
 constexpr int kPtMaxSlabs = 8192;
+constexpr int kPtAhead = 4;                                   // pages that a lane has on their way from the ring
 constexpr int kPtPageRows = SKIPKV_PAGE_ROWS;
 
 __global__ void __launch_bounds__(kPtThreads)
@@ -56,11 +57,20 @@ page_tables_kernel(int n_slabs, int max_pages, int pool, const int32_t* need, co
             if (d > 0 && !served) bad |= SKIPKV_STATUS_NO_PAGES;
         }
         if (d > 0 && served) {
-            for (int j = part * 32 + lane; j < d; j += per * 32) {
-                const int page = ring[at(head + take[s] + j)];
-                const bool ok = page >= 0 && page < pool;
-                if (!ok) bad |= SKIPKV_STATUS_BAD_TABLE;
-                row[have + j] = ok ? page : -1;
+            for (int j = part * 32 + lane; j < d; j += per * 32 * kPtAhead) {
+                int page[kPtAhead];
+#pragma unroll
+                for (int k = 0; k < kPtAhead; ++k) {
+                    const int jk = j + k * per * 32;
+                    page[k] = jk < d ? ring[at(head + take[s] + jk)] : 0;
+                }
+#pragma unroll
+                for (int k = 0; k < kPtAhead; ++k) {
+                    const int jk = j + k * per * 32;
+                    const bool ok = page[k] >= 0 && page[k] < pool;
+                    if (!ok) bad |= SKIPKV_STATUS_BAD_TABLE;
+                    if (jk < d) row[have + jk] = ok ? page[k] : -1;
+                }
             }
         } else if (d < 0) {
             for (int j = part * 32 + lane; j < -d; j += per * 32) {
@@ -83,7 +93,8 @@ page_tables_kernel(int n_slabs, int max_pages, int pool, const int32_t* need, co
     if (bad && status) atomicOr(status, bad);
 }
 
-// kHeads: KV heads of a token that a thread does (a 16-byte store where there are two)
+// kHeads: KV heads of a token that a thread does (a 16-byte store where there are two).  A CTA takes a range of tokens, a thread the same heads of
+// every few of them: it goes from one sequence to the next only now and then, and looks up a page once.
 template <int kHeads>
 __global__ void __launch_bounds__(kPtThreads)
 slot_map_kernel(int batch, int Hk, int max_pages, const int32_t* table, const int32_t* n_pages, const int32_t* start, const int32_t* new_off,
@@ -91,37 +102,56 @@ slot_map_kernel(int batch, int Hk, int max_pages, const int32_t* table, const in
     pdl_trigger();
     pdl_wait();
     const int hw = Hk / kHeads;
-    const uint32_t total = uint32_t(n_new) * uint32_t(hw);    // below 2^31
-    // a CTA takes a range of tokens, so that a thread goes from one sequence to the next only now and then
-    const uint32_t per = (total + gridDim.x - 1) / gridDim.x;
-    const uint32_t e0 = min(per * blockIdx.x, total), e1 = min(e0 + per, total);
-    int b = -1, lo = 0, hi = 0;                               // the sequence of the token before, its tokens
-    for (uint32_t e = e0 + threadIdx.x; e < e1; e += kPtThreads) {
-        const int i = int(e / uint32_t(hw)), h = int(e % uint32_t(hw)) * kHeads;
-        if (new_off == nullptr) {
-            b = i; lo = i; hi = i + 1;
-        } else if (b < 0 || i >= hi) {
-            int l = max(b, 0), r = batch;                     // the first sequence that ends behind token i
-            while (l < r) {
-                const int mid = (l + r) >> 1;
-                if (new_off[mid + 1] > i) r = mid; else l = mid + 1;
-            }
-            b = l;
-            if (b < batch) { lo = new_off[b]; hi = new_off[b + 1]; } else { lo = hi = 0x7fffffff; }
-        }
-        if (b >= batch || i < lo) continue;                   // a token of no sequence
-        int64_t v[kHeads];
+    const int tokens = hw < kPtThreads ? kPtThreads / hw : 1;                // of one pass of the CTA
+    const int first = hw < kPtThreads ? int(threadIdx.x) / hw : 0;
+    if (first >= tokens) return;
+    const int i0 = int((long long)n_new * blockIdx.x / gridDim.x), i1 = int((long long)n_new * (blockIdx.x + 1) / gridDim.x);
+    for (int hp = hw < kPtThreads ? int(threadIdx.x) % hw : int(threadIdx.x); hp < hw; hp += kPtThreads) {
+        int b = -1, lo = 0, hi = 0;                           // the sequence of the token before, its tokens
+        int at[kHeads], held[kHeads], page_at[kHeads];        // per head: its first new token, its pages, the page looked up last
+        long long page_row[kHeads];                           // and that one's first row
+        const int32_t* row[kHeads];
+        for (int i = i0 + first; i < i1; i += tokens) {
+            if (b < 0 || i >= hi) {
+                if (new_off == nullptr) {
+                    b = i; lo = i; hi = i + 1;
+                } else {
+                    int l = max(b, 0), r = batch;             // the first sequence that ends behind token i
+                    while (l < r) {
+                        const int mid = (l + r) >> 1;
+                        if (new_off[mid + 1] > i) r = mid; else l = mid + 1;
+                    }
+                    b = l;
+                    if (b < batch) { lo = new_off[b]; hi = new_off[b + 1]; } else { lo = hi = 0x7fffffff; }
+                }
+                if (b < batch) {
 #pragma unroll
-        for (int k = 0; k < kHeads; ++k) {
-            const int s = b * Hk + h + k;
-            const long long t = (long long)start[s] + (i - lo);
-            v[k] = -1;
-            if (t >= 0 && t / kPtPageRows < min(n_pages[s], max_pages))
-                v[k] = (long long)table[size_t(s) * max_pages + size_t(t / kPtPageRows)] * kPtPageRows + t % kPtPageRows;
+                    for (int k = 0; k < kHeads; ++k) {
+                        const int s = b * Hk + hp * kHeads + k;
+                        at[k] = start[s];
+                        held[k] = min(n_pages[s], max_pages);
+                        row[k] = table + size_t(s) * max_pages;
+                        page_at[k] = -1;
+                        page_row[k] = -1;
+                    }
+                }
+            }
+            if (b >= batch || i < lo) continue;               // a token of no sequence
+            int64_t v[kHeads];
+#pragma unroll
+            for (int k = 0; k < kHeads; ++k) {
+                const long long t = (long long)at[k] + (i - lo);
+                const int page = t < 0 || t >= (long long)held[k] * kPtPageRows ? -1 : int(t / kPtPageRows);
+                if (page >= 0 && page != page_at[k]) {
+                    page_at[k] = page;
+                    page_row[k] = (long long)row[k][page] * kPtPageRows;
+                }
+                v[k] = page < 0 || page_row[k] < 0 ? -1 : page_row[k] + (t & (kPtPageRows - 1));
+            }
+            int64_t* p = slots + (long long)i * Hk + hp * kHeads;
+            if (kHeads == 2) __stcs(reinterpret_cast<longlong2*>(p), make_longlong2(v[0], v[kHeads - 1]));
+            else __stcs(reinterpret_cast<long long*>(p), (long long)v[0]);
         }
-        int64_t* p = slots + (long long)i * Hk + h;
-        if (kHeads == 2) *reinterpret_cast<longlong2*>(p) = make_longlong2(v[0], v[kHeads - 1]);
-        else *p = v[0];
     }
 }
 
@@ -143,7 +173,7 @@ extern "C" int skipkv_page_tables(int32_t batch, int32_t n_kv_heads, int32_t max
     // rows of the pool, places of the ring and sums over the slabs in 32 bits
     if (int64_t(pool_pages) * SKIPKV_PAGE_ROWS > 0x7fffffff || slabs * max_pages > 0x7fffffff) return SKIPKV_ERR_UNSUPPORTED;
     const size_t smem = size_t(3 * slabs + 2) * 4;
-    const int64_t want = (slabs * 4 + kPtWarps - 1) / kPtWarps;
+    const int64_t want = (slabs * 16 + kPtWarps - 1) / kPtWarps;       // 16 warps to a slab, as far as the SMs go
     const int grid = int(want < num_sms() ? want : num_sms());
     SKIPKV_CUDA(launch_dependent(page_tables_kernel, dim3(grid), dim3(kPtThreads), smem, static_cast<cudaStream_t>(stream), int(slabs),
                                  int(max_pages), int(pool_pages), need, n_pages_in, n_pages_out, block_table, free_ring, ring_in, ring_out, status));

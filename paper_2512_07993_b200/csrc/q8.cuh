@@ -92,6 +92,14 @@ __device__ __forceinline__ uint32_t q8_round(float y0, float y1, float y2, float
     return r;
 }
 
+// int8: four values times a power of two to codes, in one rounding: 1.5 * 2^23 + the (exact) product has the nearest whole number in its low bits.
+__device__ __forceinline__ uint32_t q8_round_scaled(float2 a, float2 b, float2 k) {
+    const float2 big = make_float2(12582912.f, 12582912.f);
+    a = __ffma2_rn(a, k, big);
+    b = __ffma2_rn(b, k, big);
+    return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+}
+
 #endif  // __CUDACC__
 
 }  // namespace skipkv
