@@ -18,6 +18,7 @@ constexpr int kPtWarps = kPtThreads / 32;
 constexpr int kPtMaxSlabs = 8192;
 constexpr int kPtAhead = 4;                                   // pages that a lane has on their way from the ring
 constexpr int kPtPageRows = SKIPKV_PAGE_ROWS;
+constexpr int kPtOffsets = 1024;
 
 __global__ void __launch_bounds__(kPtThreads)
 page_tables_kernel(int n_slabs, int max_pages, int pool, const int32_t* need, const int32_t* have_in, int32_t* have_out, int32_t* table,
@@ -99,19 +100,28 @@ template <int kHeads>
 __global__ void __launch_bounds__(kPtThreads)
 slot_map_kernel(int batch, int Hk, int max_pages, const int32_t* table, const int32_t* n_pages, const int32_t* start, const int32_t* new_off,
                 int n_new, int64_t* slots) {
+    __shared__ int s_off[kPtOffsets];
     pdl_trigger();
-    pdl_wait();
     const int hw = Hk / kHeads;
     const int tokens = hw < kPtThreads ? kPtThreads / hw : 1;                // of one pass of the CTA
     const int first = hw < kPtThreads ? int(threadIdx.x) / hw : 0;
+    const uint32_t share = (uint32_t(n_new) + gridDim.x - 1) / gridDim.x;
+    const int i0 = int(min(share * blockIdx.x, uint32_t(n_new))), i1 = int(min(share * blockIdx.x + share, uint32_t(n_new)));
+    pdl_wait();
+    // the offsets are searched in shared memory where they fit: a search is a chain of reads
+    if (new_off != nullptr && batch < kPtOffsets) {
+        for (int k = threadIdx.x; k <= batch; k += kPtThreads) s_off[k] = new_off[k];
+        new_off = s_off;
+        __syncthreads();
+    }
     if (first >= tokens) return;
-    const int i0 = int((long long)n_new * blockIdx.x / gridDim.x), i1 = int((long long)n_new * (blockIdx.x + 1) / gridDim.x);
     for (int hp = hw < kPtThreads ? int(threadIdx.x) % hw : int(threadIdx.x); hp < hw; hp += kPtThreads) {
         int b = -1, lo = 0, hi = 0;                           // the sequence of the token before, its tokens
-        int at[kHeads], held[kHeads], page_at[kHeads];        // per head: its first new token, its pages, the page looked up last
-        long long page_row[kHeads];                           // and that one's first row
+        uint32_t t[kHeads], end[kHeads], page_end[kHeads];    // per head: the token, the end of the slab's pages and of the page looked up last
+        int2 page_row[kHeads];                                // that page's first row, as two words
         const int32_t* row[kHeads];
-        for (int i = i0 + first; i < i1; i += tokens) {
+        int64_t* p = slots + (long long)(i0 + first) * Hk + hp * kHeads;
+        for (int i = i0 + first; i < i1; i += tokens, p += size_t(tokens) * Hk) {
             if (b < 0 || i >= hi) {
                 if (new_off == nullptr) {
                     b = i; lo = i; hi = i + 1;
@@ -124,33 +134,35 @@ slot_map_kernel(int batch, int Hk, int max_pages, const int32_t* table, const in
                     b = l;
                     if (b < batch) { lo = new_off[b]; hi = new_off[b + 1]; } else { lo = hi = 0x7fffffff; }
                 }
-                if (b < batch) {
+                if (b < batch && i >= lo) {
 #pragma unroll
                     for (int k = 0; k < kHeads; ++k) {
-                        const int s = b * Hk + hp * kHeads + k;
-                        at[k] = start[s];
-                        held[k] = min(n_pages[s], max_pages);
+                        const int s = b * Hk + hp * kHeads + k, at = start[s];
+                        t[k] = uint32_t(at) + uint32_t(i - lo) - uint32_t(tokens);       // (one step back; below 2^32 in all)
+                        end[k] = at < 0 ? 0u : uint32_t(min(max(n_pages[s], 0), min(max_pages, 1 << 24))) * kPtPageRows;
+                        page_end[k] = 0u;
                         row[k] = table + size_t(s) * max_pages;
-                        page_at[k] = -1;
-                        page_row[k] = -1;
                     }
                 }
             }
-            if (b >= batch || i < lo) continue;               // a token of no sequence
-            int64_t v[kHeads];
+            if (b >= batch || i < lo) { hi = min(hi, i + 1); continue; }                 // a token of no sequence: look again
+            int2 v[kHeads];
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
-                const long long t = (long long)at[k] + (i - lo);
-                const int page = t < 0 || t >= (long long)held[k] * kPtPageRows ? -1 : int(t / kPtPageRows);
-                if (page >= 0 && page != page_at[k]) {
-                    page_at[k] = page;
-                    page_row[k] = (long long)row[k][page] * kPtPageRows;
+                t[k] += uint32_t(tokens);
+                v[k] = make_int2(-1, -1);
+                if (t[k] < end[k]) {
+                    if (t[k] >= page_end[k]) {
+                        const int page = row[k][t[k] / kPtPageRows];
+                        const long long r = (long long)page * kPtPageRows;
+                        page_row[k] = page < 0 ? make_int2(-1, -1) : make_int2(int(uint32_t(r)), int(r >> 32));
+                        page_end[k] = (t[k] / kPtPageRows + 1u) * kPtPageRows;
+                    }
+                    v[k] = make_int2(page_row[k].x | int(t[k] % kPtPageRows), page_row[k].y);      // (-1 stays -1)
                 }
-                v[k] = page < 0 || page_row[k] < 0 ? -1 : page_row[k] + (t & (kPtPageRows - 1));
             }
-            int64_t* p = slots + (long long)i * Hk + hp * kHeads;
-            if (kHeads == 2) __stcs(reinterpret_cast<longlong2*>(p), make_longlong2(v[0], v[kHeads - 1]));
-            else __stcs(reinterpret_cast<long long*>(p), (long long)v[0]);
+            if (kHeads == 2) __stcs(reinterpret_cast<int4*>(p), make_int4(v[0].x, v[0].y, v[kHeads - 1].x, v[kHeads - 1].y));
+            else __stcs(reinterpret_cast<int2*>(p), v[0]);
         }
     }
 }
@@ -189,7 +201,7 @@ extern "C" int skipkv_slot_map(int32_t batch, int32_t n_kv_heads, int32_t max_pa
     if (n_new == 0) return SKIPKV_OK;
     const bool two = n_kv_heads % 2 == 0 && (reinterpret_cast<uintptr_t>(slots) & 15) == 0;
     const int64_t work = int64_t(n_new) * n_kv_heads / (two ? 2 : 1);
-    const int64_t want = (work + kPtThreads - 1) / kPtThreads, most = int64_t(num_sms()) * 8;
+    const int64_t want = (work + kPtThreads - 1) / kPtThreads, most = int64_t(num_sms()) * 4;
     const int grid = int(want < most ? want : most);
     SKIPKV_CUDA(launch_dependent(two ? slot_map_kernel<2> : slot_map_kernel<1>, dim3(grid), dim3(kPtThreads), 0, static_cast<cudaStream_t>(stream),
                                  int(batch), int(n_kv_heads), int(max_pages), block_table, n_pages, start, new_off, int(n_new), slots));
