@@ -37,20 +37,25 @@ __host__ __device__ __forceinline__ int q8_room(const Q8View& v, const int32_t* 
     const long long lim = v.table ? (long long)v.max_pages * kQ8Tile : (long long)v.max_blocks << v.block_log2;
     return int(min((long long)max(cap[s / Hk], 0), lim));
 }
+// First row of slab s in a contiguous layout; -1 where it lies nowhere near the buffers (fewer than 2^31 rows).
+__host__ __device__ __forceinline__ int q8_row0(const int64_t* slab_off, const int32_t* cap, int Hk, int s) {
+    const long long row = (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk);
+    return row < 0 || row > 0x7fffff00ll ? -1 : int(row);
+}
 // Where tile j (tokens [128 j, 128 j + 128)) of slab s lies: its first row, and the place of its first block's scale.  Of its first
-// `rows` rows none may lie outside the buffers, else row = -1.
+// `rows` rows none may lie outside the buffers, else row = -1.  row0: as q8_row0 gives it (not used for a paged cache).
 struct Q8Tile { long long row; size_t scale; };
-__host__ __device__ __forceinline__ Q8Tile q8_tile(const Q8View& v, const int64_t* slab_off, const int32_t* cap, int Hk, int s, int j, int rows) {
+__host__ __device__ __forceinline__ Q8Tile q8_tile(const Q8View& v, int s, int j, int rows, int row0) {
     Q8Tile t;
     if (v.table) {
         const int page = v.table[size_t(s) * v.max_pages + j];
         t.row = (long long)page * kQ8Tile;
-        t.scale = size_t(max(page, 0)) << (7 - v.block_log2);
+        t.scale = size_t(page > 0 ? page : 0) << (7 - v.block_log2);
         if (page < 0 || t.row + kQ8Tile > v.rows) t.row = -1;
     } else {
-        t.row = (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk) + (long long)j * kQ8Tile;
+        t.row = (long long)row0 + (long long)j * kQ8Tile;
         t.scale = size_t(s) * v.max_blocks + (size_t(j) << (7 - v.block_log2));
-        if (t.row < 0 || t.row + rows > v.rows) t.row = -1;
+        if (row0 < 0 || t.row + rows > v.rows) t.row = -1;
     }
     return t;
 }

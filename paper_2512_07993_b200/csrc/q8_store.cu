@@ -92,6 +92,7 @@ q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const i
     extern __shared__ __align__(16) uint8_t qsm[];
     int* pref = reinterpret_cast<int*>(qsm);                  // [n_slabs + 1] tile prefix
     int2* span = reinterpret_cast<int2*>(qsm + ((size_t(n_slabs) + 2) / 2) * 8);     // [n_slabs] rows already there, rows afterwards
+    int* row0 = reinterpret_cast<int*>(span + n_slabs);       // [n_slabs] first rows in a contiguous layout
     __shared__ uint32_t s_wsum[kQsWarps];
     __shared__ uint32_t s_amax[2][kQsWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -102,6 +103,7 @@ q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const i
     // ---- which tiles there are
     for (int s = tid; s < n_slabs; s += kQsThreads) {
         const int room = q8_room(c, cap, Hk, s);
+        row0[s] = q8_row0(slab_off, cap, Hk, s);
         int old = 0, now = 0;
         bool bad = false;
         if (kAppend) {
@@ -132,7 +134,7 @@ q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const i
         const int old = span[s].x, now = span[s].y;
         const int j = old / kQ8Tile + (t - pref[s]);
         const int t0 = j * kQ8Tile;                           // the tile's first token
-        const Q8Tile at = q8_tile(c, slab_off, cap, Hk, s, j, min(now - t0, kQ8Tile));
+        const Q8Tile at = q8_tile(c, s, j, min(now - t0, kQ8Tile), row0[s]);
         const uint4* src = (t2 & 1) ? a.v_src : a.k_src;
         uint8_t* dst = ((t2 & 1) ? c.V : c.K) + at.row * kQ8RowBytes;
         float* scale = ((t2 & 1) ? c.v_scale : c.k_scale) + at.scale;
@@ -144,7 +146,7 @@ q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const i
             src0 = ((long long)a.new_off[b] - old) * Hk + s % Hk;
             step = Hk;
         } else {
-            src0 = (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk);
+            src0 = row0[s];
             step = 1;
             ok = ok && src0 >= 0 && src0 + now <= a.src_rows;
         }
@@ -264,7 +266,7 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
     }
     const int s = w >> 1, b = s / Hk, block = 1 << c.block_log2;
     const int lo = a.new_off ? a.new_off[b] : b, hi = a.new_off ? a.new_off[b + 1] : b + 1;
-    const long long row0 = c.table ? 0 : (long long)slab_row0(slab_off, cap, Hk, b, s % Hk);
+    const int row0 = c.table ? 0 : q8_row0(slab_off, cap, Hk, s);        // (read beside the length)
     const int old = a.len_in[s], room = q8_room(c, cap, Hk, s);
     const bool fits = old >= 0 && lo >= 0 && hi >= lo && hi <= a.n_new && (long long)old + (hi - lo) <= room;
     const int count = fits ? hi - lo : 0;
@@ -277,9 +279,7 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
         const uint2* const x = src + done * next;
         const uint2 x0 = *x;
         done += take;
-        // (q8_tile with the slab's first row at hand, which is read beside the length)
-        const Q8Tile at = c.table ? q8_tile(c, slab_off, cap, Hk, s, j, r + take)
-                                  : Q8Tile{row0 < 0 || row0 + tok + take > c.rows ? -1 : row0 + (long long)j * kQ8Tile, size_t(s) * c.max_blocks + (size_t(j) << (7 - c.block_log2))};
+        const Q8Tile at = q8_tile(c, s, j, r + take, row0);
         if (at.row < 0) {
             if (lane == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
             continue;
@@ -381,12 +381,14 @@ q8_load_kernel(int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap,
     extern __shared__ __align__(16) uint8_t qsm[];
     int* pref = reinterpret_cast<int*>(qsm);
     int* lens = pref + n_slabs + 1;
+    int* row0 = lens + n_slabs;                               // first rows in a contiguous layout
     __shared__ uint32_t s_wsum[kQsWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = gridDim.x, cta = blockIdx.x;
     pdl_trigger();
     pdl_wait();
     for (int s = tid; s < n_slabs; s += kQsThreads) {
+        row0[s] = q8_row0(slab_off, cap, Hk, s);
         const int n = kv_len[s], room = min(q8_room(c, cap, Hk, s), cap[s / Hk]);
         const bool bad = n < 0 || n > room;
         if (bad && cta == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
@@ -404,9 +406,9 @@ q8_load_kernel(int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap,
         const bool is_v = per == 2 ? (t2 & 1) != 0 : V != nullptr;
         while (pref[s + 1] <= t) ++s;
         const int j = t - pref[s], rows = min(lens[s] - j * kQ8Tile, kQ8Tile);
-        const Q8Tile at = q8_tile(c, slab_off, cap, Hk, s, j, rows);
-        const long long to = (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk) + (long long)j * kQ8Tile;
-        if (at.row < 0 || to < 0 || to + rows > dst_rows) {
+        const Q8Tile at = q8_tile(c, s, j, rows, row0[s]);
+        const long long to = (long long)row0[s] + (long long)j * kQ8Tile;
+        if (at.row < 0 || row0[s] < 0 || to + rows > dst_rows) {
             if (tid == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
             continue;
         }
@@ -467,7 +469,7 @@ template <bool kAppend>
 static int store(const skipkv_shape* shape, const skipkv_q8_cache* cache, const StoreArgs& a, long long tiles, void* ws, void* stream) {
     const int slabs = shape->batch * shape->n_kv_heads;
     if (slabs > kQ8MaxSlabs) return too_many_slabs();
-    const size_t smem = (size_t(slabs) + 2) / 2 * 8 + size_t(slabs) * 8;
+    const size_t smem = (size_t(slabs) + 2) / 2 * 8 + size_t(slabs) * 12;
     SKIPKV_CUDA(launch_dependent(cache->format == SKIPKV_Q8_E4M3 ? q8_store_kernel<SKIPKV_Q8_E4M3, kAppend> : q8_store_kernel<SKIPKV_Q8_INT8, kAppend>,
                                  dim3(store_grid(2 * tiles, 4)), dim3(kQsThreads), smem, static_cast<cudaStream_t>(stream), int(shape->batch),
                                  int(shape->n_kv_heads), slabs, shape->slab_off, shape->cap, q8_view(*cache), a, &static_cast<Header*>(ws)->status));
@@ -545,7 +547,7 @@ extern "C" int skipkv_unpack_q8(const skipkv_shape* shape, const skipkv_q8_cache
     if (slabs > kQ8MaxSlabs) return too_many_slabs();
     const long long tiles = (long long)slabs * ((shape->max_cap + kQ8Tile - 1) / kQ8Tile) * ((K ? 1 : 0) + (V ? 1 : 0));
     SKIPKV_CUDA(launch_dependent(cache->format == SKIPKV_Q8_E4M3 ? q8_load_kernel<SKIPKV_Q8_E4M3> : q8_load_kernel<SKIPKV_Q8_INT8>,
-                                 dim3(store_grid(tiles, 6)), dim3(kQsThreads), size_t(2 * slabs + 1) * 4, static_cast<cudaStream_t>(stream),
+                                 dim3(store_grid(tiles, 6)), dim3(kQsThreads), size_t(3 * slabs + 1) * 4, static_cast<cudaStream_t>(stream),
                                  int(shape->n_kv_heads), slabs, shape->slab_off, shape->cap, q8_view(*cache), kv_len, static_cast<uint4*>(K),
                                  static_cast<uint4*>(V), static_cast<long long>(shape->total_rows), &static_cast<Header*>(ws)->status));
     return SKIPKV_OK;

@@ -235,7 +235,7 @@ int main() {
             if (room < 0 || room > most || (room > 0 && room > cap[s / Hk])) { printf("room %d\n", room); return 1; }
             for (int j = 0; j * 128 < room; ++j) {
                 const int rows = room - j * 128 < 128 ? room - j * 128 : 128;
-                const Q8Tile t = q8_tile(v, off.data(), cap.data(), Hk, s, j, rows);
+                const Q8Tile t = q8_tile(v, s, j, rows, q8_row0(off.data(), cap.data(), Hk, s));
                 ++checked;
                 if (t.row < 0) { ++refused; continue; }
                 if (t.row + rows > v.rows) { printf("row %lld of %lld\n", t.row, v.rows); return 1; }
