@@ -40,15 +40,29 @@ struct StoreArgs {
     int Hq, window, slot, max_sent;
 };
 
-// The slab that holds tile t: the last one with pref <= t.
-__device__ __forceinline__ int slab_of(const int* pref, int n_slabs, int t) {
-    int lo = 0, hi = n_slabs - 1;
+// The slab that holds tile t: the last one with pref <= t; not before slab lo.
+__device__ __forceinline__ int slab_of(const int* pref, int n_slabs, int t, int lo) {
+    if (pref[lo + 1] > t) return lo;
+    int hi = n_slabs - 1;
     while (lo < hi) {
         const int mid = (lo + hi + 1) >> 1;
         if (pref[mid] <= t) lo = mid; else hi = mid - 1;
     }
     return lo;
 }
+
+// A CTA's tiles of T: every G-th, so that neighbouring CTAs work on neighbouring rows, or, where there are few, the CTA's own contiguous share,
+// which has fewer slabs to find.  80 slabs of 16K to 32K: storing 240 us against 248 with contiguous shares, loading 260 against 266; loading the keys
+// of 80 slabs of 2.1K: 16.2 with contiguous shares against 17.0.
+struct Share {
+    int first, end, step;
+    __device__ __forceinline__ Share(int T, int cta, int G) {
+        const bool few = T < 4 * G;
+        first = few ? int((long long)T * cta / G) : cta;
+        end = few ? int((long long)T * (cta + 1) / G) : T;
+        step = few ? 1 : G;
+    }
+};
 
 // Eight bf16 values times inv (a power of two) to codes.
 template <int kFmt>
@@ -122,15 +136,14 @@ q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const i
     __syncthreads();
     auto tiles_of = [&](int s) { return span[s].y > span[s].x ? (span[s].y - 1) / kQ8Tile - span[s].x / kQ8Tile + 1 : 0; };
     cta_prefix<kQsThreads>(n_slabs, tiles_of, pref, s_wsum);
-    const long long T2 = 2ll * pref[n_slabs];                 // K and V of a tile one after the other; a CTA has an equal share of them
-    const int t2_end = int(T2 * (cta + 1) / G);
+    const Share share(2 * pref[n_slabs], cta, G);             // K and V of a tile one after the other
 
     const int c16 = lane & 15, half = lane >> 4;
     const int group = 1 << (c.block_log2 - 4);                // warps to a block
-    int flip = 0, s = slab_of(pref, n_slabs, int(T2 * cta / G) >> 1);
-    for (int t2 = int(T2 * cta / G); t2 < t2_end; ++t2) {
+    int flip = 0, s = 0;
+    for (int t2 = share.first; t2 < share.end; t2 += share.step) {
         const int t = t2 >> 1;
-        while (pref[s + 1] <= t) ++s;
+        s = slab_of(pref, n_slabs, t, s);
         const int old = span[s].x, now = span[s].y;
         const int j = old / kQ8Tile + (t - pref[s]);
         const int t0 = j * kQ8Tile;                           // the tile's first token
@@ -397,14 +410,13 @@ q8_load_kernel(int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap,
     __syncthreads();
     cta_prefix<kQsThreads>(n_slabs, [&](int s) { return (lens[s] + kQ8Tile - 1) / kQ8Tile; }, pref, s_wsum);
     const int per = (K ? 1 : 0) + (V ? 1 : 0);
-    const long long T = (long long)pref[n_slabs] * per;      // a CTA has an equal share of the tiles
-    const int t2_end = int(T * (cta + 1) / G);
+    const Share share(pref[n_slabs] * per, cta, G);
     const int c16 = lane & 15, r0 = warp * 16 + (lane >> 4);
-    int t2 = int(T * cta / G), s = slab_of(pref, n_slabs, per == 2 ? t2 >> 1 : t2);
-    for (; t2 < t2_end; ++t2) {
+    int s = 0;
+    for (int t2 = share.first; t2 < share.end; t2 += share.step) {
         const int t = per == 2 ? t2 >> 1 : t2;
         const bool is_v = per == 2 ? (t2 & 1) != 0 : V != nullptr;
-        while (pref[s + 1] <= t) ++s;
+        s = slab_of(pref, n_slabs, t, s);
         const int j = t - pref[s], rows = min(lens[s] - j * kQ8Tile, kQ8Tile);
         const Q8Tile at = q8_tile(c, s, j, rows, row0[s]);
         const long long to = (long long)row0[s] + (long long)j * kQ8Tile;
