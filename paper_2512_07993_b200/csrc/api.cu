@@ -67,14 +67,14 @@ static EncodeTiledFn encode_tiled_fn() {
 }
 
 static int encode(CUtensorMap* out, const void* base, int rank, const cuuint64_t* dims, const cuuint64_t* strides,
-                  const cuuint32_t* box, CUtensorMapDataType type = CU_TENSOR_MAP_DATA_TYPE_BFLOAT16) {
+                  const cuuint32_t* box) {
     EncodeTiledFn fn = encode_tiled_fn();
     if (!fn) {
         set_error_text("cuTensorMapEncodeTiled is not available from this driver");
         return SKIPKV_ERR_CUDA;
     }
     const cuuint32_t estr[3] = {1, 1, 1};
-    const CUresult r = fn(out, type, cuuint32_t(rank), const_cast<void*>(base), dims,
+    const CUresult r = fn(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, cuuint32_t(rank), const_cast<void*>(base), dims,
                           strides, box, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
                           CU_TENSOR_MAP_L2_PROMOTION_L2_128B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE);
     if (r != CUDA_SUCCESS) {
@@ -91,13 +91,6 @@ int tmap_rows(CUtensorMap* out, const void* base, uint64_t rows, uint32_t box_ro
     const cuuint64_t strides[1] = {cuuint64_t(kRowBytes)};
     const cuuint32_t box[2] = {64, box_rows};
     return encode(out, base, 2, dims, strides, box);
-}
-
-int tmap_codes(CUtensorMap* out, const void* base, uint64_t rows, uint32_t box_rows) {
-    const cuuint64_t dims[2] = {cuuint64_t(kHeadDim), rows};
-    const cuuint64_t strides[1] = {cuuint64_t(kHeadDim)};
-    const cuuint32_t box[2] = {kHeadDim, box_rows};
-    return encode(out, base, 2, dims, strides, box, CU_TENSOR_MAP_DATA_TYPE_UINT8);
 }
 
 int tmap_groups(CUtensorMap* out, const void* base, uint64_t groups, uint32_t rows, uint32_t box_rows, uint32_t box_groups) {
