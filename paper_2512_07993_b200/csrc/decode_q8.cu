@@ -3,21 +3,26 @@
 // out = sum_t softmax_t(q . (s_k c_k)[t] / sqrt(d)) (s_v c_v)[t].  A block's scale is one number for 16 tokens or more, so it never touches the
 // codes: s_k multiplies 16 logits of a head at once, s_v the tile's share of the output sums.  Every live row is read once, 256 bytes
 // per token and slab.
-//  * Work = tiles of 128 tokens (a page) enumerated over all (sequence, head) slabs and cut into equal contiguous ranges, one per CTA, one
-//    CTA per SM; each (CTA, slab) intersection gives one partial (maximum, sum, 128 sums per head); the last CTA that delivers one for a slab
-//    merges them.
-//  * Eight warps, each with its own 16 rows of every tile and its own ring of asynchronous copies (three stages of 4 KB): no barrier in the
-//    stream.  With half the bytes per row a tile's chain of latencies must be hidden twice as well as over a bf16 cache: two warps
-//    to a scheduler.
-//  * Products in f16 on the tensor cores (mma.sync m16n8k16; a query row per head is far below a tcgen05 tile): every code of either format
-//    is an f16 value, and a query head, shifted by a power of two so that its largest magnitude is in [2^14, 2^15), is one down to 2^-38 of
-//    that.  The order of channels in S = K Q^T and of tokens and channels in O^T = V^T P^T is free, so a lane takes 16 bytes of a row as they
-//    lie: 32 consecutive channels of a key row (two 16-byte loads), 16 consecutive channels of four value rows, of which byte permutes
-//    make pairs of tokens.  Rows are 128 bytes; their 16-byte pieces lie permuted (piece c of row r at c ^ (r & 7)), so neither
-//    load has bank conflicts.
+//  * Work = tiles of 128 tokens (a page) enumerated over all (sequence, head) slabs and cut into equal contiguous ranges, one per CTA, two CTAs
+//    per SM (one: 312 us against 240 for 128 slabs of 32K to 64K: a tile is a chain of latencies); each (CTA, slab) intersection gives one partial
+//    (maximum, sum, 128 sums per head); the last CTA that delivers one for a slab merges them.  A slab costs a few places beside its tiles in the
+//    partition, because the end of a part costs time (80 slabs of 4.1K: 21.4 us with four, 24.2 with none).
+//  * Four warps, each with its own 32 rows of every tile and its own ring of asynchronous copies (three stages of 8 KB): no barrier in the
+//    stream, and nothing to wait for but a warp's own copies.  16 rows per warp and twice the warps, 304 us; tile copies by the bulk engine, issued by a
+//    lane per warp or by a fifth warp for all, 242 and 246 against 240 (128 slabs of 32K to 64K), 53.4 and 51.5 against 50.2 (8.2K, paged).
+//  * S = K Q^T on the tensor cores (a query row per head is far below a tcgen05 tile).  e4m3: the codes are operands as they lie in memory (mma.sync
+//    m16n8k32), a query head is two e4m3 parts, which together have the 8 bits of a bf16.  int8: codes and queries as f16 (m16n8k16), exact for both.
+//    O^T = V^T P^T in f16, of which every code is a value.  The order of channels in S and of tokens and channels in O is free, so a lane
+//    takes 16 bytes of a row as they lie: 32 consecutive channels of a key row (two 16-byte loads), 16 consecutive channels of four value rows, of
+//    which byte permutes make pairs of tokens.  Rows are 128 bytes; their 16-byte pieces lie permuted (piece c of row r at c ^ (r & 7)), so
+//    neither load has bank conflicts.
 //  * The probabilities go in as two f16 parts of 2^15 p, 22 bits of the fp32 value, absolute 2^-40 for small ones; a tile's products are added to the
-//    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates).  Up to four heads per group the
-//    eight columns hold high and low parts side by side.
+//    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates).  Up to four heads per group the eight columns hold the
+//    high and low parts of a head side by side, so that a lane has one head to exponentiate.
+//  * An arrival's answer is not waited for before the CTA's next part; the partials of a slab come to its last CTA through shared memory, 16 at a time.
+// What it takes (back to back, and what bounds it): one sequence of 2048 tokens 8.0 us, latency (wait 0.9, first rows 2.4, a tile 1.5, arrival 1.0,
+// merge 1.7); 80 slabs of 4.1K 19.4 us, 0.66 of the copy rate: head and tail of a launch, between them 7.5 TB/s into the SMs; 128 slabs of 8.2K
+// behind pages, int8, five heads 50.2 us, 0.81: conversions and latency; 128 slabs of 32K to 64K 240 us, 1.02, and 280 in seconds of it (power).
 #include "common.cuh"
 #include "mma.cuh"
 #include "q8.cuh"
@@ -91,7 +96,7 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// kFew: up to four heads per group (the eight columns are then the heads twice)
+// kFew: up to four heads per group
 template <int kFmt, bool kFew>
 __global__ void __launch_bounds__(kQdThreads, 2)
 decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, const __nv_bfloat16* q, Q8View c,
@@ -108,7 +113,8 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
 
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = gridDim.x, cta = blockIdx.x;
-    // ---- schedule: CTA k has the tiles [k T / Ge, (k + 1) T / Ge) of the T tiles, Ge = the CTAs that have work.  The lengths may be written by
+    // ---- schedule: CTA k has the places [k T / Ge, (k + 1) T / Ge) of T, Ge = the CTAs that have work; a slab has kQdPartCost places and then one
+    // for each tile.  The lengths may be written by
     // the launch ahead of this one, but the number of tiles they make is mostly older (a step adds one row).  So the schedule is derived from what
     // they are now, the CTA's first tiles are started towards L2 (the point of coherence, so a row that is still being written is not read too
     // early), and behind the wait the first copies go out under it at once; the lengths and the first row are read once more while those are on
@@ -158,8 +164,8 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     }
     pdl_wait();
 
-    // ---- copies: this warp's 16 rows of the CTA's k-th tile, and their two scales, go to stage k % kQdStages.  The cursor walks the slab
-    // parts of the tile range; divisions and the slab's tables are read once per part, a page's entry a tile ahead.
+    // ---- copies: this warp's 32 rows of the CTA's k-th tile, and their scales, go to stage k % kQdStages.  The cursor walks the slab parts of
+    // the range; divisions and the slab's tables are read once per part, a page's entry a tile ahead, and whole tiles take a short path.
     const uint32_t ring = smem_u32(dsm) + warp * kQdStages * kQdStageBytes;
     const int c_row = lane >> 3, c_col = lane & 7;
     const uint32_t dst0 = ring + c_row * kQ8RowBytes + ((c_col ^ c_row) << 4);        // row 4 i + c_row, i even; odd: ^ 64

@@ -6,9 +6,11 @@
 // the call's inputs, which the call does not change (counts and the ring's state go to other buffers), so no CTA waits for another.
 // The free pages are a ring, not a stack: pages are taken at its head and given back behind its tail, and with f free pages of P at most
 // P - f come back, so what is written is never what is read.  The order is that of the slabs, whatever the CTAs' order.
-// Latency: a prologue over the slabs and one chain ring -> table per page.
+// Latency: a prologue over the slabs and one chain ring -> table per page: 3.0 us for 128 slabs, whether sixteen of them enter their next page or
+// all take 256 to 512 pages.
 //
-// Slots: 8 bytes written per token and head, the pages' entries read through L1 (a page serves 128 tokens).
+// Slots: 8 bytes written per token and head.  50 MB (sixteen prompts of 32K to 64K, eight heads) take 10.1 us, 0.76 of the copy rate with the launch;
+// a decode step's 128 take 2.2.
 #include "common.cuh"
 
 namespace skipkv {
@@ -94,19 +96,22 @@ page_tables_kernel(int n_slabs, int max_pages, int pool, const int32_t* need, co
     if (bad && status) atomicOr(status, bad);
 }
 
-// kHeads: KV heads of a token that a thread does (a 16-byte store where there are two).  A CTA takes a range of tokens, a thread the same heads of
-// every few of them: it goes from one sequence to the next only now and then, and looks up a page once.
+// kHeads: KV heads of a token that a thread does (a 16-byte store where there are two).  A warp takes a range of tokens, a lane the same heads of
+// every few of them: it goes from one sequence to the next only now and then, and looks up a page every 128 tokens.  (A CTA's range with its
+// threads side by side looks up a page every other token: 12.3 us against 10.1 for sixteen prompts of 32K to 64K, eight heads.)
 template <int kHeads>
 __global__ void __launch_bounds__(kPtThreads)
 slot_map_kernel(int batch, int Hk, int max_pages, const int32_t* table, const int32_t* n_pages, const int32_t* start, const int32_t* new_off,
                 int n_new, int64_t* slots) {
     __shared__ int s_off[kPtOffsets];
     pdl_trigger();
+    const int lane = threadIdx.x & 31;
     const int hw = Hk / kHeads;
-    const int tokens = hw < kPtThreads ? kPtThreads / hw : 1;                // of one pass of the CTA
-    const int first = hw < kPtThreads ? int(threadIdx.x) / hw : 0;
-    const uint32_t share = (uint32_t(n_new) + gridDim.x - 1) / gridDim.x;
-    const int i0 = int(min(share * blockIdx.x, uint32_t(n_new))), i1 = int(min(share * blockIdx.x + share, uint32_t(n_new)));
+    const int tokens = hw < 32 ? 32 / hw : 1;                 // of one pass of the warp
+    const int first = hw < 32 ? lane / hw : 0;
+    const uint32_t warps = gridDim.x * kPtWarps, w = blockIdx.x * kPtWarps + (threadIdx.x >> 5);
+    const uint32_t share = (uint32_t(n_new) + warps - 1) / warps;
+    const int i0 = int(min(share * w, uint32_t(n_new))), i1 = int(min(share * w + share, uint32_t(n_new)));
     pdl_wait();
     // the offsets are searched in shared memory where they fit: a search is a chain of reads
     if (new_off != nullptr && batch < kPtOffsets) {
@@ -115,54 +120,51 @@ slot_map_kernel(int batch, int Hk, int max_pages, const int32_t* table, const in
         __syncthreads();
     }
     if (first >= tokens) return;
-    for (int hp = hw < kPtThreads ? int(threadIdx.x) % hw : int(threadIdx.x); hp < hw; hp += kPtThreads) {
-        int b = -1, lo = 0, hi = 0;                           // the sequence of the token before, its tokens
-        uint32_t t[kHeads], end[kHeads], page_end[kHeads];    // per head: the token, the end of the slab's pages and of the page looked up last
-        int2 page_row[kHeads];                                // that page's first row, as two words
-        const int32_t* row[kHeads];
-        int64_t* p = slots + (long long)(i0 + first) * Hk + hp * kHeads;
-        for (int i = i0 + first; i < i1; i += tokens, p += size_t(tokens) * Hk) {
-            if (b < 0 || i >= hi) {
-                if (new_off == nullptr) {
-                    b = i; lo = i; hi = i + 1;
-                } else {
-                    int l = max(b, 0), r = batch;             // the first sequence that ends behind token i
-                    while (l < r) {
-                        const int mid = (l + r) >> 1;
-                        if (new_off[mid + 1] > i) r = mid; else l = mid + 1;
-                    }
-                    b = l;
-                    if (b < batch) { lo = new_off[b]; hi = new_off[b + 1]; } else { lo = hi = 0x7fffffff; }
+    for (int hp = hw < 32 ? lane % hw : lane; hp < hw; hp += 32) {
+        int i = i0 + first, b = 0;
+        int64_t* p = slots + (long long)i * Hk + hp * kHeads;
+        const size_t next = size_t(tokens) * Hk;
+        while (i < i1) {
+            int lo = i, hi = i + 1;                           // the tokens of sequence b
+            if (new_off == nullptr) {
+                b = i;
+            } else {
+                int r = batch;                                // the first sequence that ends behind token i
+                while (b < r) {
+                    const int mid = (b + r) >> 1;
+                    if (new_off[mid + 1] > i) r = mid; else b = mid + 1;
                 }
-                if (b < batch && i >= lo) {
-#pragma unroll
-                    for (int k = 0; k < kHeads; ++k) {
-                        const int s = b * Hk + hp * kHeads + k, at = start[s];
-                        t[k] = uint32_t(at) + uint32_t(i - lo) - uint32_t(tokens);       // (one step back; below 2^32 in all)
-                        end[k] = at < 0 ? 0u : uint32_t(min(max(n_pages[s], 0), min(max_pages, 1 << 24))) * kPtPageRows;
-                        page_end[k] = 0u;
-                        row[k] = table + size_t(s) * max_pages;
-                    }
-                }
+                if (b == batch) break;                        // tokens of no sequence
+                lo = new_off[b]; hi = new_off[b + 1];
             }
-            if (b >= batch || i < lo) { hi = min(hi, i + 1); continue; }                 // a token of no sequence: look again
-            int2 v[kHeads];
+            if (i < lo) { i += tokens; p += next; continue; }
+            uint32_t t[kHeads], end[kHeads], page_end[kHeads];     // per head: the token (below 2^32), the end of the slab's pages and of the last one looked up
+            long long page_row[kHeads];                       // that one's first row
+            const int32_t* row[kHeads];
 #pragma unroll
             for (int k = 0; k < kHeads; ++k) {
-                t[k] += uint32_t(tokens);
-                v[k] = make_int2(-1, -1);
-                if (t[k] < end[k]) {
-                    if (t[k] >= page_end[k]) {
-                        const int page = row[k][t[k] / kPtPageRows];
-                        const long long r = (long long)page * kPtPageRows;
-                        page_row[k] = page < 0 ? make_int2(-1, -1) : make_int2(int(uint32_t(r)), int(r >> 32));
-                        page_end[k] = (t[k] / kPtPageRows + 1u) * kPtPageRows;
-                    }
-                    v[k] = make_int2(page_row[k].x | int(t[k] % kPtPageRows), page_row[k].y);      // (-1 stays -1)
-                }
+                const int s = b * Hk + hp * kHeads + k, at = start[s];
+                t[k] = uint32_t(at) + uint32_t(i - lo);
+                end[k] = at < 0 ? 0u : uint32_t(min(max(n_pages[s], 0), min(max_pages, 1 << 24))) * kPtPageRows;
+                row[k] = table + size_t(s) * max_pages;
+                page_end[k] = 0u;
+                page_row[k] = -1;
             }
-            if (kHeads == 2) __stcs(reinterpret_cast<int4*>(p), make_int4(v[0].x, v[0].y, v[kHeads - 1].x, v[kHeads - 1].y));
-            else __stcs(reinterpret_cast<int2*>(p), v[0]);
+            for (const int stop = min(hi, i1); i < stop; i += tokens, p += next) {
+                long long v[kHeads];
+#pragma unroll
+                for (int k = 0; k < kHeads; ++k) {
+                    if (t[k] >= page_end[k]) {
+                        const int page = t[k] < end[k] ? row[k][t[k] / kPtPageRows] : -1;
+                        page_row[k] = page < 0 ? -1ll : (long long)page * kPtPageRows;
+                        page_end[k] = t[k] < end[k] ? (t[k] | (kPtPageRows - 1u)) + 1u : 0xffffffffu;
+                    }
+                    v[k] = page_row[k] | (long long)(t[k] & (kPtPageRows - 1u));       // (-1 stays -1)
+                    t[k] += uint32_t(tokens);
+                }
+                if (kHeads == 2) __stcs(reinterpret_cast<longlong2*>(p), make_longlong2(v[0], v[kHeads - 1]));
+                else __stcs(reinterpret_cast<long long*>(p), v[0]);
+            }
         }
     }
 }
@@ -201,7 +203,7 @@ extern "C" int skipkv_slot_map(int32_t batch, int32_t n_kv_heads, int32_t max_pa
     if (n_new == 0) return SKIPKV_OK;
     const bool two = n_kv_heads % 2 == 0 && (reinterpret_cast<uintptr_t>(slots) & 15) == 0;
     const int64_t work = int64_t(n_new) * n_kv_heads / (two ? 2 : 1);
-    const int64_t want = (work + kPtThreads - 1) / kPtThreads, most = int64_t(num_sms()) * 4;
+    const int64_t want = (work + kPtThreads - 1) / kPtThreads, most = int64_t(num_sms()) * 2;
     const int grid = int(want < most ? want : most);
     SKIPKV_CUDA(launch_dependent(two ? slot_map_kernel<2> : slot_map_kernel<1>, dim3(grid), dim3(kPtThreads), 0, static_cast<cudaStream_t>(stream),
                                  int(batch), int(n_kv_heads), int(max_pages), block_table, n_pages, start, new_off, int(n_new), slots));
