@@ -114,7 +114,8 @@ int skipkv_set_wait_limit(void* ws, uint32_t polls, void* stream);
 int skipkv_wait_probe(void* ws, void* stream);
 
 /* Read and clear the device status word.  Synchronises `stream`.  *status_bits (host,
- * nullable) receives the SKIPKV_STATUS_* bits; returns SKIPKV_ERR_TIMEOUT if a wait ran out. */
+ * nullable) receives the SKIPKV_STATUS_* bits; returns SKIPKV_ERR_TIMEOUT if a wait ran out, SKIPKV_ERR_INVALID_ARG if a
+ * table or a length was inconsistent; SKIPKV_STATUS_NOT_FINITE alone is no error. */
 int skipkv_status(void* ws, void* stream, uint32_t* status_bits);
 
 /* Text of the last CUDA error seen by this library on the calling thread (host string). */
@@ -441,7 +442,8 @@ int skipkv_decode_attn_static(const skipkv_shape* shape, const void* q, const vo
  * code of its sign, a NaN as 0, and SKIPKV_STATUS_NOT_FINITE is raised.  Codes and scales are the same bits from run to run.
  * The reading calls take any positive scales.  Rows that lie outside the buffers (a page that is not in [0, rows / SKIPKV_PAGE_ROWS),
  * a slab that reaches beyond `rows`) are neither read nor written: SKIPKV_STATUS_BAD_TABLE is raised, and attention goes on
- * without them.
+ * without them.  Two slabs must not share a page that a call writes (reading a shared one is fine).  None of these calls waits for anything on
+ * the GPU but the work before it on the stream: the wait limit does not concern them.
  */
 #define SKIPKV_Q8_E4M3 0
 #define SKIPKV_Q8_INT8 1
@@ -509,6 +511,7 @@ int skipkv_decode_attn_q8(const skipkv_shape* shape, const skipkv_q8_cache* cach
  * skipkv_unpack_q8 -- the live rows of an 8-bit cache as bf16 slabs, for the calls that read 16 bits: scoring and compaction
  * of a layer (then skipkv_pack_q8 again).  K[row of (b, h, t)] = bf16(s_k c_k), rounded to nearest even, for t < kv_len[b][h]; V the
  * same.  K, V: device bf16, contiguous slabs of `shape`, shape->total_rows rows; either may be NULL.  Other rows are not written.
+ * A length beyond the slab's room is taken as the room, one below zero as zero, and SKIPKV_STATUS_BAD_TABLE is raised.
  */
 int skipkv_unpack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const int32_t* kv_len, void* K, void* V,
                      void* ws, void* stream);

@@ -155,6 +155,72 @@ def test_captured_tables_and_slots(B):
     assert int(sv.status) == 0 and sv.state.tolist() == [sv.head, sv.free]
 
 
+@pytest.mark.parametrize("pause", [True, False])
+def test_pages_slots_append_and_attention_behind_one_another(B, pause):
+    """A decode loop in which every call's input is what the call before it wrote, with and without a pause between them: pages are taken as
+    slabs grow, and rows of a pool that no slab holds stay as they were."""
+    bt, hk, max_pages, pool = 3, 2, 4, 30
+    sv = Server(B, bt, hk, max_pages, pool, 9)
+    K, V = (torch.full((pool * 128, 128), -128, dtype=torch.int8, device="cuda") for _ in range(2))
+    ks, vs = (torch.full((pool, 4), float("nan"), device="cuda") for _ in range(2))
+    cache = B.make_q8_cache(K, V, ks, vs, 32, sv.table)
+    off16 = torch.zeros(bt, dtype=torch.int64, device="cuda")
+    cap = torch.full((bt,), max_pages * 128, dtype=torch.int32, device="cuda")
+    shape = B.make_shape(bt, hk * 2, hk, 128, 1, 0, 1, max_pages * 128, off16, cap, pool * 128)
+    ws = torch.empty(B.skipkv_workspace_bytes(shape), dtype=torch.uint8, device="cuda")
+    B.skipkv_workspace_init(shape, ws)
+    g = torch.Generator(device="cuda").manual_seed(4)
+    k, v = (torch.randn(260, bt, hk, 128, generator=g, device="cuda").bfloat16() for _ in range(2))
+    q = torch.randn(260, bt, hk * 2, 128, generator=g, device="cuda").bfloat16()
+    out, slots = torch.zeros_like(q), torch.full((260, bt, hk), -5, dtype=torch.int64, device="cuda")
+    n, n2 = sv.n, sv.n2
+    state, state2 = sv.state, sv.state2
+    kv = torch.zeros(261, bt, hk, dtype=torch.int32, device="cuda")
+    kv[0] = torch.tensor([[100, 120], [0, 127], [128, 250]], dtype=torch.int32)
+    need = kv[0].clone()
+    B.skipkv_page_tables(bt, hk, max_pages, pool, need, n, n2, sv.table, sv.ring, state, state2, sv.status)
+    n, n2, state, state2 = n2, n, state2, state
+    torch.cuda.synchronize()
+    for i in range(260):
+        torch.add(kv[i], 1, out=need)
+        for call in (lambda: B.skipkv_page_tables(bt, hk, max_pages, pool, need, n, n2, sv.table, sv.ring, state, state2, sv.status),
+                     lambda: B.skipkv_slot_map(bt, hk, max_pages, sv.table, n2, kv[i], None, bt, slots[i]),
+                     lambda: B.skipkv_append_q8(shape, cache, k[i], v[i], None, bt, kv[i], kv[i + 1], ws),
+                     lambda: B.skipkv_decode_attn_q8(shape, cache, q[i], kv[i + 1], out[i], None, None, None, None, ws)):
+            call()
+            if pause:
+                torch.cuda.synchronize()
+        n, n2, state, state2 = n2, n, state2, state
+    torch.cuda.synchronize()
+    # (the tokens before the first step were never stored: junk codes of scale NaN, so those slabs' results are NaN; slab (1, 0) began empty)
+    assert int(sv.status) == 0 and B.skipkv_status(ws, raise_on_error=False) == 0
+    assert kv[260].tolist() == [[360, 380], [260, 387], [388, 510]] and n.tolist() == [[3, 3], [3, 4], [4, 4]]
+    assert state.tolist()[1] == pool - 21
+    table, sl = sv.table.cpu().numpy(), slots.cpu().numpy()
+    held = {int(p) for b in range(bt) for h in range(hk) for p in table[b, h, :int(n[b, h])]}
+    assert len(held) == 21
+    for i in (0, 1, 27, 28, 127, 128, 259):
+        for b in range(bt):
+            for h in range(hk):
+                t = int(kv[0, b, h]) + i
+                assert sl[i, b, h] == table[b, h, t // 128] * 128 + t % 128
+    free = torch.ones(pool, dtype=torch.bool)
+    free[list(held)] = False
+    assert bool((K.view(pool, 128, 128)[free.cuda()] == -128).all()) and bool(torch.isnan(ks[free.cuda()]).all())
+    host = [[np.zeros((512, 128), np.uint8), np.zeros(16)] for _ in range(2)]
+    for j, x in enumerate((k, v)):
+        for i in range(260):
+            oracle.q8_append(*host[j], i, x[i, 1, 0][None].double().cpu().numpy(), 32, "int8")
+            if i in (0, 130, 259):
+                rows = oracle.q8_rows(*host[j], i + 1, 32, "int8")
+                if j == 0:
+                    keys = getattr(sv, "keys", {})
+                    keys[i] = rows
+                    sv.keys = keys
+                else:
+                    check_attention(type("C", (), dict(hk=1, slabs=1, rows64=[[sv.keys[i]], [rows]])), q[i, 1:2, :2], out[i, 1:2, :2])
+
+
 def test_slots_scatter_a_prompt_into_a_bf16_pool(B):
     """Pages for prompts, their slots as an index for torch's copy, and the paged bf16 attention over the result."""
     bt, hk, group, lens = 3, 2, 4, [300, 1, 129]

@@ -70,7 +70,7 @@ def attend(c, q, **kw):
 
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("paged", [False, True])
-@pytest.mark.parametrize("group", [1, 2, 3, 4, 5, 7, 8])
+@pytest.mark.parametrize("group", [1, 2, 3, 4, 5, 6, 7, 8])
 def test_attention(B, fmt, paged, group):
     """Lengths around the rows of a warp and of a page, none and one among them, other ones in every head."""
     lens = [[0, 1, 15], [16, 17, 127], [128, 129, 300], [1000, 2, 255]]
@@ -120,6 +120,96 @@ def test_attention_with_a_nan_in_one_head(B):
     q = queries(c, 8, 7)
     out = attend(c, q).float()
     assert bool(torch.isnan(out[0, :4, 5]).all()) and int(torch.isnan(out).sum()) == 4
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("value", [float("inf"), float("-inf"), float("nan")])
+def test_attention_with_a_query_that_is_not_finite(B, fmt, value):
+    """Its head is NaN, as the products would make it; the others are what they are."""
+    c = filled(B, [[200, 200]], [200], 2, fmt, 16, False, 9, n_q=12)
+    q = queries(c, 12, 7)
+    q[0, 4, 17] = value
+    out = attend(c, q)
+    assert bool(torch.isnan(out[0, 4].float()).all())
+    q[0, 4, 17] = 0
+    keep = torch.arange(12, device="cuda") != 4
+    assert torch.equal(out[:, keep], attend(c, q)[:, keep])
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+def test_attention_over_as_many_slabs_as_there_may_be(B, fmt):
+    lens = np.random.default_rng(1).integers(0, 4, (1024, 8))
+    c = Cache(B, lens, [3] * 1024, 8, fmt, 16, False, 2, n_q=8)
+    x = values(c.r, c.rows16).cuda()
+    B.skipkv_pack_q8(c.shape, c.cache, x, x, c.kv_len, c.ws)
+    back = torch.zeros_like(x)
+    B.skipkv_unpack_q8(c.shape, c.cache, c.kv_len, back, None, c.ws)
+    q = queries(c, 8, 6)
+    out = attend(c, q)
+    assert c.status() == 0
+    host = back.double().cpu().numpy()
+    c.rows64 = [[host[c.row0[s]:c.row0[s] + int(lens.reshape(-1)[s])] for s in range(c.slabs)]] * 2
+    check_attention(c, q, out)
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_two_streams_with_a_workspace_each(B, paged):
+    """Calls over two caches that run at the same time give what they give alone."""
+    cs = [filled(B, [[3000, 33], [200, 1500]], [3000, 1500], 2, "e4m3", 64, paged, 20 + i, n_q=8) for i in range(2)]
+    qs = [queries(c, 8, 30 + i) for i, c in enumerate(cs)]
+    alone = [attend(c, q) for c, q in zip(cs, qs)]
+    outs = [[torch.zeros_like(qs[i]) for _ in range(20)] for i in range(2)]
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    torch.cuda.synchronize()
+    for k in range(20):
+        for i in range(2):
+            B.skipkv_decode_attn_q8(cs[i].shape, cs[i].cache, qs[i], cs[i].kv_len, outs[i][k], None, None, None, None, cs[i].ws, streams[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        assert cs[i].status() == 0
+        for o in outs[i]:
+            assert torch.equal(o, alone[i])
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("replayed", [False, True])
+def test_steps_behind_one_another_see_the_lengths_that_the_step_before_left(B, paged, replayed):
+    """Append and attention without a pause, lengths that cross rows, blocks and tiles: the same bits as with a pause behind every call.  (The
+    attention derives its work from the lengths before the append ahead of it has finished, and has to notice.)"""
+    lens = [[120, 3], [250, 384]]
+    runs = []
+    for pause in (True, False):
+        c = filled(B, lens, [700, 700], 2, "int8", 16, paged, 5, n_q=8)
+        r = np.random.default_rng(6)
+        k, v = (bf16(r.normal(0, 1, (150, 2, 2, 128)) * np.exp2(np.arange(150) % 5)[:, None, None, None]).cuda() for _ in range(2))
+        q = bf16(r.normal(0, 1, (150, 2, 8, 128))).cuda()
+        out = torch.zeros_like(q)
+        a, b = c.kv_len.clone(), torch.zeros_like(c.kv_len)
+
+        def step(i):
+            src, dst = (a, b) if i % 2 == 0 else (b, a)
+            B.skipkv_append_q8(c.shape, c.cache, k[i], v[i], None, 2, src, dst, c.ws)
+            if pause:
+                torch.cuda.synchronize()
+            B.skipkv_decode_attn_q8(c.shape, c.cache, q[i], dst, out[i], None, None, None, None, c.ws)
+            if pause:
+                torch.cuda.synchronize()
+
+        if replayed and not pause:
+            torch.cuda.synchronize()
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                for i in range(150):
+                    step(i)
+            g.replay()
+        else:
+            for i in range(150):
+                step(i)
+        torch.cuda.synchronize()
+        assert c.status() == 0 and (a if 150 % 2 == 0 else b).tolist() == [[n + 150 for n in x] for x in lens]
+        runs.append((out, c.K.clone(), c.V.clone()))
+    for x, y in zip(*runs):
+        assert torch.equal(x, y)
 
 
 @pytest.mark.parametrize("paged", [False, True])
@@ -304,6 +394,36 @@ def test_append(B, fmt, paged, block):
         assert np.array_equal(b.cpu().numpy().reshape(-1), lens)
         for s in range(c.slabs):
             same(c, s, int(lens[s]), [host[0][0][s], host[1][0][s]], [host[0][1][s], host[1][1][s]])
+        a, b = b, a
+    c.untouched(lens)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("block", [16, 128])
+def test_append_no_more_rows_than_sequences(B, fmt, paged, block):
+    """A few rows in all, however they fall to the sequences: across blocks and pages, with scales that grow, NaN and infinities among them."""
+    hk, bt = 2, 7
+    c = Cache(B, np.zeros((bt, hk)), [300] * bt, hk, fmt, block, paged, 11)
+    host = [([np.zeros((400, 128), np.uint8) for _ in range(c.slabs)], [np.zeros(-(-400 // block)) for _ in range(c.slabs)]) for _ in range(2)]
+    lens = np.zeros(c.slabs, np.int32)
+    a, b = torch.zeros(bt, hk, dtype=torch.int32, device="cuda"), torch.full((bt, hk), -1, dtype=torch.int32, device="cuda")
+    parts = [[120, 125, 14, 15, 16, 250, 0], [7, 0, 0, 0, 0, 0, 0], [0, 5, 1, 1, 0, 0, 0], [0, 0, 3, 4, 0, 0, 0], [0] * 7, [0, 0, 0, 0, 0, 6, 1], [1] * 7,
+             [2, 0, 2, 0, 2, 0, 1]]
+    for i, part in enumerate(parts):
+        off = np.concatenate([[0], np.cumsum(part)])
+        x = [values(c.r, max(int(off[-1]), 1) * hk, wild=i == 5).double().numpy().reshape(-1, hk, 128) * 2.0 ** (i % 5 - 2) for _ in range(2)]
+        x = [bf16(y) for y in x]
+        B.skipkv_append_q8(c.shape, c.cache, x[0].cuda(), x[1].cuda(), torch.from_numpy(off.astype(np.int32)).cuda(), int(off[-1]), a, b, c.ws)
+        torch.cuda.synchronize()
+        assert c.status() == (8 if i == 5 else 0)
+        for s in range(c.slabs):
+            q, h = divmod(s, hk)
+            for k in range(2):
+                n = oracle.q8_append(host[k][0][s], host[k][1][s], int(lens[s]), x[k][int(off[q]):int(off[q + 1]), h].double().numpy(), block, fmt)
+            lens[s] = n
+            same(c, s, n, [host[0][0][s], host[1][0][s]], [host[0][1][s], host[1][1][s]])
+        assert np.array_equal(b.cpu().numpy().reshape(-1), lens)
         a, b = b, a
     c.untouched(lens)
 
