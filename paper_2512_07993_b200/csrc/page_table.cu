@@ -6,11 +6,11 @@
 // the call's inputs, which the call does not change (counts and the ring's state go to other buffers), so no CTA waits for another.
 // The free pages are a ring, not a stack: pages are taken at its head and given back behind its tail, and with f free pages of P at most
 // P - f come back, so what is written is never what is read.  The order is that of the slabs, whatever the CTAs' order.
-// Latency: a prologue over the slabs and one chain ring -> table per page: 3.0 us for 128 slabs, whether sixteen of them enter their next page or
+// Latency: a prologue over the slabs and one chain ring -> table per page: 3.2 us for 128 slabs, whether sixteen of them enter their next page or
 // all take 256 to 512 pages.
 //
 // Slots: 8 bytes written per token and head.  50 MB (sixteen prompts of 32K to 64K, eight heads) take 10.1 us, 0.76 of the copy rate with the launch;
-// a decode step's 128 take 2.2.
+// a decode step's 128 take 2.4.
 #include "common.cuh"
 
 namespace skipkv {
@@ -31,8 +31,8 @@ page_tables_kernel(int n_slabs, int max_pages, int pool, const int32_t* need, co
     int* delta = give + n_slabs + 1;                          // [n_slabs] pages wanted beyond those held
     __shared__ uint32_t s_wsum[kPtWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, cta = blockIdx.x;
-    pdl_trigger();
     pdl_wait();
+    pdl_trigger();                                            // (see the slots)
     uint32_t bad = 0;
     const int head = ring_in[0], free0 = ring_in[1];
     const bool ring_ok = head >= 0 && head < pool && free0 >= 0 && free0 <= pool;
@@ -104,7 +104,6 @@ __global__ void __launch_bounds__(kPtThreads)
 slot_map_kernel(int batch, int Hk, int max_pages, const int32_t* table, const int32_t* n_pages, const int32_t* start, const int32_t* new_off,
                 int n_new, int64_t* slots) {
     __shared__ int s_off[kPtOffsets];
-    pdl_trigger();
     const int lane = threadIdx.x & 31;
     const int hw = Hk / kHeads;
     const int tokens = hw < 32 ? 32 / hw : 1;                 // of one pass of the warp
@@ -113,6 +112,9 @@ slot_map_kernel(int batch, int Hk, int max_pages, const int32_t* table, const in
     const uint32_t share = (uint32_t(n_new) + warps - 1) / warps;
     const int i0 = int(min(share * w, uint32_t(n_new))), i1 = int(min(share * w + share, uint32_t(n_new)));
     pdl_wait();
+    // Triggered behind the wait, here and in the tables: at most one call behind this one has CTAs on the SMs while it runs.  With two of them there
+    // the CTAs of slots crowd on the SMs that were free first: 26 us for tables and slots of those prompts in turn, against 14.1.
+    pdl_trigger();
     // the offsets are searched in shared memory where they fit: a search is a chain of reads
     if (new_off != nullptr && batch < kPtOffsets) {
         for (int k = threadIdx.x; k <= batch; k += kPtThreads) s_off[k] = new_off[k];
