@@ -440,10 +440,11 @@ int skipkv_decode_attn_static(const skipkv_shape* shape, const void* q, const vo
  * What the storing calls write: s is a power of two, the smallest that brings the largest finite magnitude of the block's rows to
  * at most 448 (E4M3) or 127 (INT8), 2^-100 at least; c = value / s rounded to nearest even.  An infinity is stored as the largest
  * code of its sign, a NaN as 0, and SKIPKV_STATUS_NOT_FINITE is raised.  Codes and scales are the same bits from run to run.
- * The reading calls take any positive scales.  Rows that lie outside the buffers (a page that is not in [0, rows / SKIPKV_PAGE_ROWS),
- * a slab that reaches beyond `rows`) are neither read nor written: SKIPKV_STATUS_BAD_TABLE is raised, and attention goes on
- * without them.  Two slabs must not share a page that a call writes (reading a shared one is fine).  None of these calls waits for anything on
- * the GPU but the work before it on the stream: the wait limit does not concern them.
+ * The reading calls take any positive scales, an append to a block those up to 2^122.  Rows that lie outside the buffers (a page that is
+ * not in [0, rows / SKIPKV_PAGE_ROWS), a slab that reaches beyond `rows`) are neither read nor written: SKIPKV_STATUS_BAD_TABLE is
+ * raised, and attention goes on without them.  Two slabs must not share a page that a call writes (reading a shared one is fine).  None of
+ * these calls waits for anything on the GPU but the work before it on the stream: the wait limit does not concern them.  At most 8192
+ * slabs, and fewer than 2^30 scales in a table of contiguous slabs or entries in a block table (SKIPKV_ERR_UNSUPPORTED).
  */
 #define SKIPKV_Q8_E4M3 0
 #define SKIPKV_Q8_INT8 1
@@ -542,7 +543,8 @@ int skipkv_page_tables(int32_t batch, int32_t n_kv_heads, int32_t max_pages, int
  * t % SKIPKV_PAGE_ROWS with t = start[b][h] + i - new_off[b], for new_off[b] <= i < new_off[b + 1]; -1 where the slab holds no
  * page for t (t / SKIPKV_PAGE_ROWS >= n_pages[b][h], or a negative entry).  An index for the caller's own copies into the pool.  start, n_pages: device
  * int32 [batch][Hk].  new_off: device int32 [batch + 1], ascending, or NULL: token i belongs to sequence i.  slots: device int64
- * [n_new][Hk]; entries of tokens that belong to no sequence are not written.  n_new = 0 does nothing.
+ * [n_new][Hk], fewer than 2^31 - 255 entries (SKIPKV_ERR_UNSUPPORTED); those of tokens that belong to no sequence are not written.
+ * n_new = 0 does nothing.
  */
 int skipkv_slot_map(int32_t batch, int32_t n_kv_heads, int32_t max_pages, const int32_t* block_table, const int32_t* n_pages,
                     const int32_t* start, const int32_t* new_off, int32_t n_new, int64_t* slots, void* stream);

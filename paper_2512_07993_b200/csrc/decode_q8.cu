@@ -23,6 +23,8 @@
 // What it takes (back to back, and what bounds it): one sequence of 2048 tokens 8.0 us, latency (wait 0.9, first rows 2.4, a tile 1.5, arrival 1.0,
 // merge 1.7); 80 slabs of 4.1K 19.4 us, 0.66 of the copy rate: head and tail of a launch, between them 7.5 TB/s into the SMs; 128 slabs of 8.2K
 // behind pages, int8, five heads 50.2 us, 0.81: conversions and latency; 128 slabs of 32K to 64K 240 us, 1.02, and 280 in seconds of it (power).
+#include <type_traits>
+
 #include "common.cuh"
 #include "mma.cuh"
 #include "q8.cuh"
@@ -40,6 +42,8 @@ constexpr int kQdRingBytes = kQdWarps * kQdStages * kQdStageBytes;
 constexpr int kQdMaxGrid = 512;
 constexpr int kQdPartCost = 4;                                // what a slab costs beside its tiles, in tiles: the end of a part
 constexpr int kQdPrefetch = 3;                                // tiles that a CTA starts towards L2 before it may read the cache
+constexpr int kQdTableSlabs = 1024;                           // from so many slabs on their table has a launch of its own: 1024 of 300 rows 29.8 us
+                                                              // with it and 31.7 without, 512 of 200 rows 15.9 and 15.3
 constexpr int kQdSumStride = kHeadDim + 4;                    // (of a column's sums in shared memory)
 static_assert(kQdStageBytes >= 8 * kQdSumStride * 4, "a warp's sums of a segment fit into a stage");
 constexpr int kQdMergeParts = kQdStageBytes / (kHeadDim * 4);   // partials of a head that are merged at a time
@@ -96,15 +100,30 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void* src) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 
-// kFew: up to four heads per group
-template <int kFmt, bool kFew>
+// The lengths and the partition's prefix sum of many slabs (q8_table_kernel).
+struct QdSlabs {
+    struct Raw { int len, cap; };
+    Q8View c;
+    const int32_t *kv_len, *cap;
+    int Hk;
+    int* lens;
+    __device__ __forceinline__ Raw load(int s) const { return {kv_len[s], cap[s / Hk]}; }
+    __device__ __forceinline__ int count(int s, const Raw& r) const {
+        const int len = min(max(r.len, 0), q8_room(c, r.cap));
+        lens[s] = len;
+        return len ? (len + kQ8Tile - 1) / kQ8Tile + kQdPartCost : 0;
+    }
+};
+
+// kFew: up to four heads per group.  kTable: many slabs, whose table the launch ahead has made.
+template <int kFmt, bool kFew, bool kTable>
 __global__ void __launch_bounds__(kQdThreads, 2)
 decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, const __nv_bfloat16* q, Q8View c,
                  const int32_t* kv_len, __nv_bfloat16* out, uint32_t* status, uint32_t* dec_cnt, float* dec_part, int d_model,
-                 __nv_bfloat16* hidden, const __nv_bfloat16* steer_vec, const float* alpha, const uint8_t* flag) {
+                 __nv_bfloat16* hidden, const __nv_bfloat16* steer_vec, const float* alpha, const uint8_t* flag, int* slab_table) {
     extern __shared__ __align__(128) uint8_t dsm[];
     const int n = Hq / Hk;                                                   // heads per group
-    int* pref = reinterpret_cast<int*>(dsm + kQdRingBytes);                  // [n_slabs + 1] tile prefix
+    int* pref = kTable ? slab_table : reinterpret_cast<int*>(dsm + kQdRingBytes);      // [n_slabs + 1] tile prefix
     int* lens = pref + n_slabs + 1;                                          // [n_slabs]
     __shared__ __align__(16) float s_scale[kQdWarps][kQdStages][4];          // of each stage's key rows (two groups of 16), then of its value rows
     __shared__ float2 s_ml[kQdWarps][kMaxGroup];                             // a segment's maxima and sums
@@ -121,27 +140,50 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     // their way, and only if the schedule is another one is it derived again.  (These reads bypass L1, which could keep the earlier value.)
     const int s_per = (n_slabs + kQdThreads - 1) / kQdThreads;
     const int s_lo = min(tid * s_per, n_slabs), s_hi = min(s_lo + s_per, n_slabs);
-    auto length = [&](int s) { return min(max(__ldcg(kv_len + s), 0), q8_room(c, cap, Hk, s)); };
+    auto length = [&](int s) { return min(max(__ldcg(kv_len + s), 0), q8_room(c, __ldcg(cap + s / Hk))); };
+    auto slab_row = [&](int s) { return (long long)(__ldcg(reinterpret_cast<const long long*>(slab_off) + s / Hk) * Hk + (long long)(s % Hk) * __ldcg(cap + s / Hk)); };
     auto tiles = [](int rows) { return (rows + kQ8Tile - 1) / kQ8Tile; };
+    if (kTable) {
+        pdl_wait();
+    } else {
 #pragma unroll 1
-    for (int s = s_lo; s < s_hi; ++s) lens[s] = length(s);
+        for (int s = s_lo; s < s_hi; ++s) lens[s] = length(s);
+    }
     int T, Ge, t_begin, t_end, slab;
     auto derive = [&]() {
-        cta_prefix<kQdThreads>(n_slabs, [&](int s) { return lens[s] ? tiles(lens[s]) + kQdPartCost : 0; }, pref, s_wsum);
+        if (!kTable) cta_prefix<kQdThreads>(n_slabs, [&](int s) { return lens[s] ? tiles(lens[s]) + kQdPartCost : 0; }, pref, s_wsum);
         T = pref[n_slabs];
         Ge = min(G, T);
         auto first_of = [&](int k) { return T < (1 << 22) ? int(uint32_t(k) * uint32_t(T) / uint32_t(Ge)) : int((long long)k * T / Ge); };
         t_begin = cta < Ge ? first_of(cta) : T;
         t_end = cta < Ge ? first_of(cta + 1) : T;
-        slab = 0;
-        int hi = n_slabs - 1;                             // slab holding place t_begin: the last one with pref <= t_begin
-        while (slab < hi) {
-            const int mid = (slab + hi + 1) >> 1;
-            if (pref[mid] <= t_begin) slab = mid; else hi = mid - 1;
+        slab = 0;                                         // slab holding place t_begin: the last one with pref <= t_begin
+        if (kTable) {                                     // (two reads, not one for each halving)
+            slab = max(__syncthreads_count(tid * s_per < n_slabs && pref[min(tid * s_per, n_slabs)] <= t_begin) - 1, 0) * s_per;
+            slab += max(__syncthreads_count(tid < s_per && slab + tid < n_slabs && pref[min(slab + tid, n_slabs)] <= t_begin) - 1, 0);
+        } else {
+            int hi = n_slabs - 1;
+            while (slab < hi) {
+                const int mid = (slab + hi + 1) >> 1;
+                if (pref[mid] <= t_begin) slab = mid; else hi = mid - 1;
+            }
         }
         t_begin = max(t_begin, pref[slab] + kQdPartCost);
     };
     derive();
+    // the slab that has place t, from one that ends at or before it on
+    auto slab_at = [&](int s, int t) {
+        if (!kTable) {
+            while (pref[s + 1] <= t) ++s;
+            return s;
+        }
+        if (pref[++s + 1] > t) return s;                  // (slabs without rows lie between)
+        int step = 1;
+        while (s + step < n_slabs && pref[s + step] <= t) { s += step; step *= 2; }
+        for (; step; step >>= 1)
+            if (s + step < n_slabs && pref[s + step] <= t) s += step;
+        return s;
+    };
     auto cta_of = [&](int place) {
         return T < (1 << 22) ? int((uint32_t(place + 1) * uint32_t(Ge) - 1u) / uint32_t(T)) : int(((long long)(place + 1) * Ge - 1) / T);
     };
@@ -149,10 +191,10 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     auto first_row = [&]() {
         if (t_begin >= t_end) return 0ll;
         if (c.table) return (long long)__ldcg(c.table + size_t(slab) * c.max_pages + (t_begin - pref[slab] - kQdPartCost));
-        return (long long)(__ldcg(reinterpret_cast<const long long*>(slab_off) + slab / Hk) * Hk + (long long)(slab % Hk) * __ldcg(cap + slab / Hk));
+        return slab_row(slab);
     };
     long long row_first = first_row();
-    if (tid < 2 * kQdPrefetch && t_begin + (tid >> 1) < min(t_end, pref[slab + 1])) {
+    if (!kTable && tid < 2 * kQdPrefetch && t_begin + (tid >> 1) < min(t_end, pref[slab + 1])) {
         const int t = t_begin + (tid >> 1), j = t - pref[slab] - kQdPartCost, rows = min(lens[slab] - j * kQ8Tile, kQ8Tile);
         const long long row = !c.table ? row_first + (long long)j * kQ8Tile
                                        : (t == t_begin ? row_first : (long long)__ldcg(c.table + size_t(slab) * c.max_pages + j)) * kQ8Tile;
@@ -162,7 +204,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             asm volatile("prefetch.global.L2 [%0];" ::"l"(((tid & 1) ? c.v_scale : c.k_scale) + at));
         }
     }
-    pdl_wait();
+    if (!kTable) pdl_wait();
 
     // ---- copies: this warp's 32 rows of the CTA's k-th tile, and their scales, go to stage k % kQdStages.  The cursor walks the slab parts of
     // the range; divisions and the slab's tables are read once per part, a page's entry a tile ahead, and whole tiles take a short path.
@@ -212,7 +254,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             if (++p_stage == kQdStages) p_stage = 0;
         } else if (p_t < t_end) {
             if (p_t == p_end) {
-                while (pref[p_slab + 1] <= p_t) ++p_slab;
+                if (pref[p_slab + 1] <= p_t) p_slab = slab_at(p_slab, p_t);
                 p_end = pref[p_slab + 1];
                 p_t = max(p_t, pref[p_slab] + kQdPartCost);
                 if (p_t >= t_end) { p_t = p_end = t_end; cp_async_commit(); return; }
@@ -221,7 +263,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                     p_table = c.table + size_t(p_slab) * c.max_pages + j;
                     p_page = p_t == t_begin ? int(row_first) : __ldcg(p_table);
                 } else {
-                    const long long row0 = p_t == t_begin ? row_first : (long long)slab_row0(slab_off, cap, Hk, p_slab / Hk, p_slab % Hk);
+                    const long long row0 = p_t == t_begin ? row_first : slab_row(p_slab);
                     p_row0 = int(row0 < 0 || row0 > c.rows ? c.rows : row0);
                 }
             }
@@ -282,10 +324,10 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     };
     int q_slab = slab;
     if (t_begin < t_end) fetch_q(slab);
-    const int len_again = s_lo < s_hi ? length(s_lo) : 0;
-    const long long row_again = first_row();
+    const int len_again = !kTable && s_lo < s_hi ? length(s_lo) : 0;
+    const long long row_again = kTable ? 0 : first_row();
 #pragma unroll 1
-    for (int attempt = 0;; ++attempt) {
+    for (int attempt = kTable ? 1 : 0;; ++attempt) {
 #pragma unroll 1
         for (int k = 0; k < kQdStages - 1; ++k) issue_next(attempt == 0);
         if (attempt) break;
@@ -377,7 +419,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     uint32_t pend_old = 0;
     while (true) {
         // -------------------------------------------------------------- one (CTA, slab) segment
-        while (t < t_end && pref[slab + 1] <= t) ++slab;
+        if (t < t_end && pref[slab + 1] <= t) slab = slab_at(slab, t);
         if (t < t_end) t = max(t, pref[slab] + kQdPartCost);
         const bool more = t < t_end;
         if (!more && pend < 0) break;
@@ -674,11 +716,15 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     cp_async_wait<0>();
     // slabs with no row to attend to: zeros (owned round-robin)
 #pragma unroll 1
-    for (int s = cta; s < n_slabs; s += G) {
-        if (lens[s]) continue;
-        __nv_bfloat16* o = out + size_t(s) * n * kHeadDim;
+    for (int k = 0; cta + G * k < n_slabs; k += 32) {
+        const int mine = cta + G * (k + lane);
+        uint32_t empty = __ballot_sync(0xffffffffu, mine < n_slabs && lens[min(mine, n_slabs - 1)] == 0);
 #pragma unroll 1
-        for (int i = tid; i < n * kHeadDim; i += kQdThreads) o[i] = __float2bfloat16_rn(0.f);
+        for (; empty; empty &= empty - 1) {
+            __nv_bfloat16* o = out + size_t(cta + G * (k + __ffs(int(empty)) - 1)) * n * kHeadDim;
+#pragma unroll 1
+            for (int i = tid; i < n * kHeadDim; i += kQdThreads) o[i] = __float2bfloat16_rn(0.f);
+        }
     }
 }
 
@@ -690,28 +736,35 @@ extern "C" int skipkv_decode_attn_q8(const skipkv_shape* shape, const skipkv_q8_
                                      void* out, void* hidden, const void* steer_vec, const float* alpha, const uint8_t* flag, void* ws,
                                      void* stream) {
     if (int rc = check_shape(shape)) return rc;
-    if (int rc = check_q8(cache)) return rc;
+    if (int rc = check_q8(shape, cache)) return rc;
     if (!q || !kv_len || !out) return SKIPKV_ERR_INVALID_ARG;
     if (hidden && (!steer_vec || !alpha || !flag || shape->d_model <= 0)) return SKIPKV_ERR_INVALID_ARG;
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return SKIPKV_ERR_WORKSPACE;
     if ((reinterpret_cast<uintptr_t>(q) & 15) || (reinterpret_cast<uintptr_t>(out) & 3)) return SKIPKV_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(hidden) | reinterpret_cast<uintptr_t>(steer_vec)) & 15) return SKIPKV_ERR_INVALID_ARG;
     const WsLayout L = make_layout(*shape);
-    if (L.slabs > kQ8MaxSlabs) {
-        set_error_text("skipkv_decode_attn_q8: batch * n_kv_heads above 8192");
-        return SKIPKV_ERR_UNSUPPORTED;
-    }
-    if (!cache->block_table && int64_t(L.slabs) * cache->max_blocks > 0x7fffffff) return SKIPKV_ERR_UNSUPPORTED;      // places of scales in 32 bits
     uint8_t* w = static_cast<uint8_t*>(ws);
-    const size_t smem = size_t(kQdRingBytes) + size_t(2 * L.slabs + 1) * 4;
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const bool table = L.slabs >= kQdTableSlabs;
+    int* slab_table = reinterpret_cast<int*>(w + L.slab_table);
+    if (table) {
+        const QdSlabs slabs{q8_view(*cache), kv_len, shape->cap, int(shape->n_kv_heads), slab_table + L.slabs + 1};
+        SKIPKV_CUDA(launch_dependent(q8_table_kernel<QdSlabs>, dim3(1), dim3(kQ8TableThreads), 0, st, int(L.slabs), slabs, slab_table));
+    }
+    const size_t smem = size_t(kQdRingBytes) + (table ? 0 : size_t(2 * L.slabs + 1) * 4);
     const int grid = 2 * num_sms() < kQdMaxGrid ? 2 * num_sms() : kQdMaxGrid;
-    const auto kernel = cache->format == SKIPKV_Q8_E4M3 ? (L.group <= 4 ? decode_q8_kernel<SKIPKV_Q8_E4M3, true> : decode_q8_kernel<SKIPKV_Q8_E4M3, false>)
-                                                        : (L.group <= 4 ? decode_q8_kernel<SKIPKV_Q8_INT8, true> : decode_q8_kernel<SKIPKV_Q8_INT8, false>);
-    SKIPKV_CUDA(launch_dependent(kernel, dim3(grid), dim3(kQdThreads), smem, static_cast<cudaStream_t>(stream), int(shape->batch),
-                                 int(shape->n_q_heads), int(shape->n_kv_heads), int(L.slabs), shape->slab_off, shape->cap,
-                                 static_cast<const __nv_bfloat16*>(q), q8_view(*cache), kv_len, static_cast<__nv_bfloat16*>(out),
-                                 &reinterpret_cast<Header*>(w + L.header)->status, reinterpret_cast<uint32_t*>(w + L.dec_cnt),
-                                 reinterpret_cast<float*>(w + L.dec_part), int(shape->d_model), static_cast<__nv_bfloat16*>(hidden),
-                                 static_cast<const __nv_bfloat16*>(steer_vec), alpha, flag));
+    auto run = [&](auto kernel) {
+        return launch_dependent(kernel, dim3(grid), dim3(kQdThreads), smem, st, int(shape->batch), int(shape->n_q_heads), int(shape->n_kv_heads),
+                                int(L.slabs), shape->slab_off, shape->cap, static_cast<const __nv_bfloat16*>(q), q8_view(*cache), kv_len,
+                                static_cast<__nv_bfloat16*>(out), &reinterpret_cast<Header*>(w + L.header)->status,
+                                reinterpret_cast<uint32_t*>(w + L.dec_cnt), reinterpret_cast<float*>(w + L.dec_part), int(shape->d_model),
+                                static_cast<__nv_bfloat16*>(hidden), static_cast<const __nv_bfloat16*>(steer_vec), alpha, flag, slab_table);
+    };
+    auto pick = [&](auto fmt) {
+        constexpr int kFmt = decltype(fmt)::value;
+        if (L.group <= 4) return table ? run(decode_q8_kernel<kFmt, true, true>) : run(decode_q8_kernel<kFmt, true, false>);
+        return table ? run(decode_q8_kernel<kFmt, false, true>) : run(decode_q8_kernel<kFmt, false, false>);
+    };
+    SKIPKV_CUDA(cache->format == SKIPKV_Q8_E4M3 ? pick(std::integral_constant<int, SKIPKV_Q8_E4M3>()) : pick(std::integral_constant<int, SKIPKV_Q8_INT8>()));
     return SKIPKV_OK;
 }

@@ -201,7 +201,7 @@ extern "C" int skipkv_slot_map(int32_t batch, int32_t n_kv_heads, int32_t max_pa
     if (batch <= 0 || n_kv_heads <= 0 || max_pages <= 0 || n_new < 0) return SKIPKV_ERR_INVALID_ARG;
     if (!block_table || !n_pages || !start || (!slots && n_new > 0)) return SKIPKV_ERR_INVALID_ARG;
     if (!new_off && n_new > batch) return SKIPKV_ERR_INVALID_ARG;
-    if (int64_t(batch) * n_kv_heads > 0x7fffffff || int64_t(n_new) * n_kv_heads > 0x7fffffff) return SKIPKV_ERR_UNSUPPORTED;
+    if (int64_t(batch) * n_kv_heads > 0x7fffffff || int64_t(n_new) * n_kv_heads > 0x7fffff00) return SKIPKV_ERR_UNSUPPORTED;
     if (n_new == 0) return SKIPKV_OK;
     const bool two = n_kv_heads % 2 == 0 && (reinterpret_cast<uintptr_t>(slots) & 15) == 0;
     const int64_t work = int64_t(n_new) * n_kv_heads / (two ? 2 : 1);

@@ -8,11 +8,13 @@
 //   int32_t*, int64_t*, float*, uint8_t*, uint32_t*           contiguous device tensor of that type (uint32_t: int32), or None
 //   void*                                        contiguous bfloat16 device tensor, or None
 //   int32_t, float                               numbers
-// and the trailing void* parameters are the workspace (any type) and the stream (None: the current stream).
+// and the trailing void* parameters are the workspace (any type) and the stream (None: the current stream).  The entries marked kHere
+// also refuse tensors of another device than the current one.
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
 #include <ATen/core/Tensor.h>
+#include <c10/cuda/CUDAFunctions.h>
 #include <c10/cuda/CUDAStream.h>
 #include <torch/csrc/autograd/python_variable.h>
 
@@ -99,13 +101,25 @@ bool stream_ptr(PyObject* o, void** out) {
     return true;
 }
 
-template <auto kFn, bool kWs, typename... A, size_t... I>
+// every tensor among the arguments is on the current device
+bool all_here(PyObject* const* args, Py_ssize_t nargs) {
+    const int dev = c10::cuda::current_device();
+    for (Py_ssize_t i = 0; i < nargs; ++i)
+        if (THPVariable_Check(args[i])) {
+            const at::Tensor& t = THPVariable_Unpack(args[i]);
+            if (t.is_cuda() && t.get_device() != dev) return fail_value("a tensor is on another device than the current one");
+        }
+    return true;
+}
+
+template <auto kFn, bool kWs, bool kHere, typename... A, size_t... I>
 PyObject* invoke(int (*)(A...), std::index_sequence<I...>, PyObject* const* args, Py_ssize_t nargs) {
     constexpr size_t n = sizeof...(A);                    // the stream is the last parameter, the workspace (if any) the one before
     if (nargs != Py_ssize_t(n)) {
         PyErr_Format(PyExc_TypeError, "%zd arguments expected, got %zd", Py_ssize_t(n), nargs);
         return nullptr;
     }
+    if (kHere && !all_here(args, nargs)) return nullptr;
     std::tuple<std::remove_cv_t<A>...> v{};
     void* stream = nullptr;
     const bool ok = ([&] {
@@ -123,10 +137,10 @@ PyObject* invoke(int (*)(A...), std::index_sequence<I...>, PyObject* const* args
 template <typename F> struct Arity;
 template <typename... A> struct Arity<int (*)(A...)> { static constexpr size_t value = sizeof...(A); };
 
-template <auto kFn, bool kWs = true>
+template <auto kFn, bool kWs = true, bool kHere = false>
 PyObject* entry(PyObject*, PyObject* const* args, Py_ssize_t nargs) {
     try {
-        return invoke<kFn, kWs>(kFn, std::make_index_sequence<Arity<decltype(kFn)>::value>{}, args, nargs);
+        return invoke<kFn, kWs, kHere>(kFn, std::make_index_sequence<Arity<decltype(kFn)>::value>{}, args, nargs);
     } catch (const std::exception& e) {
         PyErr_SetString(PyExc_RuntimeError, e.what());
         return nullptr;
@@ -139,9 +153,10 @@ PyMethodDef methods[] = {
     ENTRY(skipkv_select_fill_red), ENTRY(skipkv_compact), ENTRY(skipkv_compact_fill), ENTRY(skipkv_compact_paged),
     ENTRY(skipkv_token_redundancy), ENTRY(skipkv_decode_attn), ENTRY(skipkv_decode_attn_paged), ENTRY(skipkv_decode_step),
     ENTRY(skipkv_decode_step_paged), ENTRY(skipkv_append), ENTRY(skipkv_append_step), ENTRY(skipkv_decode_attn_static, false),
-    ENTRY(skipkv_table_step, false), ENTRY(skipkv_steer, false), ENTRY(skipkv_pack_q8), ENTRY(skipkv_append_q8),
-    ENTRY(skipkv_append_step_q8), ENTRY(skipkv_decode_attn_q8), ENTRY(skipkv_unpack_q8), ENTRY(skipkv_page_tables, false),
-    ENTRY(skipkv_slot_map, false),
+    ENTRY(skipkv_table_step, false), ENTRY(skipkv_steer, false),
+    ENTRY(skipkv_pack_q8, true, true), ENTRY(skipkv_append_q8, true, true), ENTRY(skipkv_append_step_q8, true, true),
+    ENTRY(skipkv_decode_attn_q8, true, true), ENTRY(skipkv_unpack_q8, true, true), ENTRY(skipkv_page_tables, false, true),
+    ENTRY(skipkv_slot_map, false, true),
     {nullptr, nullptr, 0, nullptr}};
 #undef ENTRY
 

@@ -28,19 +28,23 @@ inline Q8View q8_view(const skipkv_q8_cache& c) {
     v.max_blocks = c.max_blocks; v.max_pages = c.max_pages;
     return v;
 }
-int check_q8(const skipkv_q8_cache* c);       // SKIPKV_OK or an error code (shape-independent checks)
+int check_q8(const skipkv_shape* s, const skipkv_q8_cache* c);      // SKIPKV_OK or an error code
 
 #ifdef __CUDACC__
 
-// Rows that slab s has room for.
-__host__ __device__ __forceinline__ int q8_room(const Q8View& v, const int32_t* cap, int Hk, int s) {
+// Rows that a slab of `cap` rows has room for.
+__host__ __device__ __forceinline__ int q8_room(const Q8View& v, int cap) {
     const long long lim = v.table ? (long long)v.max_pages * kQ8Tile : (long long)v.max_blocks << v.block_log2;
-    return int(min((long long)max(cap[s / Hk], 0), lim));
+    return int(min((long long)max(cap, 0), lim));
+}
+__host__ __device__ __forceinline__ int q8_room(const Q8View& v, const int32_t* cap, int Hk, int s) { return q8_room(v, cap[s / Hk]); }
+__host__ __device__ __forceinline__ int q8_row0(int64_t off, int cap, int Hk, int s) {
+    const long long row = (long long)(size_t(off) * Hk + size_t(s % Hk) * cap);
+    return row < 0 || row > 0x7fffff00ll ? -1 : int(row);
 }
 // First row of slab s in a contiguous layout; -1 where it lies nowhere near the buffers (fewer than 2^31 rows).
 __host__ __device__ __forceinline__ int q8_row0(const int64_t* slab_off, const int32_t* cap, int Hk, int s) {
-    const long long row = (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk);
-    return row < 0 || row > 0x7fffff00ll ? -1 : int(row);
+    return q8_row0(slab_off[s / Hk], cap[s / Hk], Hk, s);
 }
 // Where tile j (tokens [128 j, 128 j + 128)) of slab s lies: its first row, and the place of its first block's scale.  Of its first
 // `rows` rows none may lie outside the buffers, else row = -1.  row0: as q8_row0 gives it (not used for a paged cache).
@@ -103,6 +107,51 @@ __device__ __forceinline__ uint32_t q8_round_scaled(float2 a, float2 b, float2 k
     a = __ffma2_rn(a, k, big);
     b = __ffma2_rn(b, k, big);
     return __byte_perm(__byte_perm(__float_as_uint(a.x), __float_as_uint(a.y), 0x0040), __byte_perm(__float_as_uint(b.x), __float_as_uint(b.y), 0x0040), 0x5410);
+}
+
+// Many slabs: one CTA, in a launch of its own, makes the prefix sum over the slabs' tiles that the CTAs of the launch behind it else make each for
+// itself, which takes the longer the more slabs there are, and shared memory that costs resident CTAs.  8192 slabs of 500 rows: attention 226 us
+// with it against 460, storing 531 against 1050, loading 580 against 694.
+constexpr int kQ8TableThreads = 1024;
+constexpr int kQ8TableEach = kQ8MaxSlabs / kQ8TableThreads;
+
+// Slabs::load(s) reads what the GPU memory says of slab s, Slabs::count(s, ...) makes its number of it.  pref: [n_slabs + 1].
+template <typename Slabs>
+__global__ void __launch_bounds__(kQ8TableThreads)
+q8_table_kernel(int n_slabs, Slabs slabs, int* pref) {
+    __shared__ int s_wsum[kQ8TableThreads / 32];
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    pdl_wait();
+    pdl_trigger();                                            // (behind the wait: the CTAs of the launch behind wait on the SMs as it is)
+    const int per = (n_slabs + kQ8TableThreads - 1) / kQ8TableThreads, s0 = tid * per;
+    typename Slabs::Raw raw[kQ8TableEach];
+#pragma unroll
+    for (int i = 0; i < kQ8TableEach; ++i)
+        if (i < per && s0 + i < n_slabs) raw[i] = slabs.load(s0 + i);
+    int cnt[kQ8TableEach], local = 0;
+#pragma unroll
+    for (int i = 0; i < kQ8TableEach; ++i) {
+        cnt[i] = i < per && s0 + i < n_slabs ? slabs.count(s0 + i, raw[i]) : 0;
+        local += cnt[i];
+    }
+    int inc = local;
+#pragma unroll
+    for (int d = 1; d < 32; d <<= 1) {
+        const int x = __shfl_up_sync(0xffffffffu, inc, d);
+        if (lane >= d) inc += x;
+    }
+    if (lane == 31) s_wsum[warp] = inc;
+    __syncthreads();
+    int run = lane < warp ? s_wsum[lane] : 0;
+#pragma unroll
+    for (int d = 16; d; d >>= 1) run += __shfl_xor_sync(0xffffffffu, run, d);
+    run += inc - local;
+#pragma unroll
+    for (int i = 0; i < kQ8TableEach; ++i) {
+        if (i < per && s0 + i < n_slabs) pref[s0 + i] = run;
+        run += cnt[i];
+    }
+    if (tid == kQ8TableThreads - 1) pref[n_slabs] = run;
 }
 
 #endif  // __CUDACC__

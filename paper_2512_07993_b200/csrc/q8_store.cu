@@ -11,6 +11,8 @@
 // tokens of one slab and tensor, aligned to 128 tokens of the slab, so a block is never shared by two CTAs; all slabs' tiles are
 // enumerated from the lengths on the GPU (ragged lengths cost nothing), K and V in turn.  A warp takes 16 rows, 16 lanes to a row (16 bytes of bf16,
 // 8 bytes of codes each), all its loads in flight together; maxima meet in shared memory where a block has more than 16 rows.
+#include <type_traits>
+
 #include "common.cuh"
 #include "q8.cuh"
 
@@ -19,6 +21,8 @@ namespace skipkv {
 constexpr int kQsThreads = 256;
 constexpr int kQsWarps = kQsThreads / 32;
 static_assert(kQsWarps * 16 == kQ8Tile, "a warp takes 16 rows of a tile");
+constexpr int kQsTableSlabs = 2048;           // from so many slabs on their table has a launch of its own: storing 1024 slabs of 300 rows 45.2 us with it and
+                                              // 42.9 without, 2048 of 1000 rows 256.5 and 256.9
 
 // Where the rows come from, and what else a decode step writes.
 struct StoreArgs {
@@ -100,13 +104,56 @@ __device__ __forceinline__ int held_exp(float s) {
     return int(bits >> 23) - 127 + ((bits & 0x7fffffu) != 0u);
 }
 
-template <int kFmt, bool kAppend>
+// What a slab is to get: old rows that it has, now rows afterwards, row0 its first row in a contiguous layout.
+struct Span { int old, now, row0; bool bad; };
+template <bool kAppend>
+struct StoreSlabs {
+    struct Raw { int lo, hi, len, cap; int64_t off; };
+    Q8View c;
+    const int64_t* slab_off;
+    const int32_t *cap, *new_off, *len_in;
+    int32_t* len_out;
+    uint32_t* status;
+    int n_new, Hk;
+    __device__ __forceinline__ Raw load(int s) const {
+        const int b = s / Hk;
+        return {kAppend ? new_off[b] : 0, kAppend ? new_off[b + 1] : 0, len_in[s], cap[b], slab_off[b]};
+    }
+    __device__ __forceinline__ Span span(int s, const Raw& r) const {
+        const int room = q8_room(c, r.cap);
+        Span x;
+        x.row0 = q8_row0(r.off, r.cap, Hk, s);
+        if (kAppend) {
+            x.old = r.len;
+            x.bad = r.len < 0 || r.lo < 0 || r.hi < r.lo || r.hi > n_new || (long long)r.len + (r.hi - r.lo) > room;
+            x.now = x.bad ? r.len : r.len + (r.hi - r.lo);
+        } else {
+            x.old = 0;
+            x.bad = r.len < 0 || r.len > room || r.len > r.cap;
+            x.now = x.bad ? 0 : r.len;
+        }
+        return x;
+    }
+    static __device__ __forceinline__ int tiles(int old, int now) { return now > old ? (now - 1) / kQ8Tile - old / kQ8Tile + 1 : 0; }
+    __device__ __forceinline__ int count(int s, const Raw& r) const {                  // (q8_table_kernel)
+        const Span x = span(s, r);
+        if (x.bad) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+        if (kAppend) len_out[s] = x.now;
+        return tiles(x.old, x.now);
+    }
+};
+
+// kTable: many slabs, whose tile prefix the launch ahead has made.
+template <int kFmt, bool kAppend, bool kTable>
 __global__ void __launch_bounds__(kQsThreads, 4)
-q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, Q8View c, StoreArgs a, uint32_t* status) {
+q8_store_kernel(int n_slabs, StoreSlabs<kAppend> slabs, StoreArgs a, const int* slab_table) {
     extern __shared__ __align__(16) uint8_t qsm[];
     int* pref = reinterpret_cast<int*>(qsm);                  // [n_slabs + 1] tile prefix
-    int2* span = reinterpret_cast<int2*>(qsm + ((size_t(n_slabs) + 2) / 2) * 8);     // [n_slabs] rows already there, rows afterwards
-    int* row0 = reinterpret_cast<int*>(span + n_slabs);       // [n_slabs] first rows in a contiguous layout
+    int2* span = reinterpret_cast<int2*>(qsm + ((size_t(n_slabs) + 2) / 2) * 8);     // (not kTable) [n_slabs] rows already there, rows afterwards
+    int* row0 = reinterpret_cast<int*>(span + n_slabs);       // (not kTable) [n_slabs] first rows in a contiguous layout
+    const Q8View& c = slabs.c;
+    const int Hk = slabs.Hk;
+    uint32_t* const status = slabs.status;
     __shared__ uint32_t s_wsum[kQsWarps];
     __shared__ uint32_t s_amax[2][kQsWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
@@ -115,27 +162,20 @@ q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const i
     pdl_wait();
 
     // ---- which tiles there are
-    for (int s = tid; s < n_slabs; s += kQsThreads) {
-        const int room = q8_room(c, cap, Hk, s);
-        row0[s] = q8_row0(slab_off, cap, Hk, s);
-        int old = 0, now = 0;
-        bool bad = false;
-        if (kAppend) {
-            const int b = s / Hk, lo = a.new_off[b], hi = a.new_off[b + 1];
-            old = a.len_in[s];
-            bad = old < 0 || lo < 0 || hi < lo || hi > a.n_new || (long long)old + (hi - lo) > room;
-            now = bad ? old : old + (hi - lo);
-        } else {
-            now = a.len_in[s];
-            bad = now < 0 || now > room || now > cap[s / Hk];
-            if (bad) now = 0;
+    if (kTable) {
+#pragma unroll 4
+        for (int s = tid; s <= n_slabs; s += kQsThreads) pref[s] = slab_table[s];
+        __syncthreads();
+    } else {
+        for (int s = tid; s < n_slabs; s += kQsThreads) {
+            const Span x = slabs.span(s, slabs.load(s));
+            if (x.bad && cta == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+            row0[s] = x.row0;
+            span[s] = make_int2(x.old, x.now);
         }
-        if (bad && cta == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
-        span[s] = make_int2(old, now);
+        __syncthreads();
+        cta_prefix<kQsThreads>(n_slabs, [&](int s) { return slabs.tiles(span[s].x, span[s].y); }, pref, s_wsum);
     }
-    __syncthreads();
-    auto tiles_of = [&](int s) { return span[s].y > span[s].x ? (span[s].y - 1) / kQ8Tile - span[s].x / kQ8Tile + 1 : 0; };
-    cta_prefix<kQsThreads>(n_slabs, tiles_of, pref, s_wsum);
     const Share share(2 * pref[n_slabs], cta, G);             // K and V of a tile one after the other
 
     const int c16 = lane & 15, half = lane >> 4;
@@ -144,10 +184,11 @@ q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const i
     for (int t2 = share.first; t2 < share.end; t2 += share.step) {
         const int t = t2 >> 1;
         s = slab_of(pref, n_slabs, t, s);
-        const int old = span[s].x, now = span[s].y;
+        const Span x_s = kTable ? slabs.span(s, slabs.load(s)) : Span{span[s].x, span[s].y, row0[s], false};
+        const int old = x_s.old, now = x_s.now;
         const int j = old / kQ8Tile + (t - pref[s]);
         const int t0 = j * kQ8Tile;                           // the tile's first token
-        const Q8Tile at = q8_tile(c, s, j, min(now - t0, kQ8Tile), row0[s]);
+        const Q8Tile at = q8_tile(c, s, j, min(now - t0, kQ8Tile), x_s.row0);
         const uint4* src = (t2 & 1) ? a.v_src : a.k_src;
         uint8_t* dst = ((t2 & 1) ? c.V : c.K) + at.row * kQ8RowBytes;
         float* scale = ((t2 & 1) ? c.v_scale : c.k_scale) + at.scale;
@@ -159,7 +200,7 @@ q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const i
             src0 = ((long long)a.new_off[b] - old) * Hk + s % Hk;
             step = Hk;
         } else {
-            src0 = row0[s];
+            src0 = x_s.row0;
             step = 1;
             ok = ok && src0 >= 0 && src0 + now <= a.src_rows;
         }
@@ -256,28 +297,36 @@ q8_store_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const i
         }
     }
 
-    if constexpr (kAppend) {
+    if constexpr (kAppend && !kTable) {
         for (int i = cta * kQsThreads + tid; i < n_slabs; i += G * kQsThreads) a.len_out[i] = span[i].y;
     }
 }
 
-// A row to each slab, or a few: a warp to a slab and tensor, four channels to a lane, block after block.  Nothing but latency: lengths and
-// offsets are requested together, the rows and the scale behind them (paged: behind the page's entry); the codes that a block has are touched only
-// where its scale grows.  80 slabs: 1.7 us in a graph, against 5.9 with the general kernel, which enumerates tiles first.
+// A row to each slab, or a few: kParts warps to a slab and tensor, four channels to a lane, a warp with every kParts-th block.  Nothing but latency:
+// lengths and offsets are requested together, the rows and the scale behind them (paged: behind the page's entry); the codes that a block has are
+// touched only where its scale grows.  A call takes it with up to four rows per sequence: the general kernel enumerates tiles first and has one step
+// of the work (a tile) go through each CTA after the other.  Eight heads, us here / there: 16 sequences with a row each 2.0 / 5.7, four each 2.2 / 5.7;
+// 256 sequences 3.4 / 33 and 6.6 / 33.  Where one sequence has all the rows (of 16 to 64, or 256 sequences) it is 3.0 / 4.5, 7.2 / 4.6 and, with
+// 1024 rows, 28 / 8: the offsets are on the GPU, and that is the rarer case.  Four parts cost more than they give where there is a row to a
+// sequence: 256 sequences 6.3 against 3.4.
 constexpr int kQoThreads = 128;
+constexpr int kQoMost = 4;                                     // rows per sequence, on average
+constexpr int kQoParts = 4;                                    // with more rows than sequences
+constexpr int kQoRows = 8;                                     // rows of new tokens on their way at a time
+constexpr int kQoHeld = 16;                                    // and of rows that a block had
 
-template <int kFmt>
+template <int kFmt, int kParts>
 __global__ void __launch_bounds__(kQoThreads)
 q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, Q8View c, StoreArgs a, uint32_t* status) {
     const int lane = threadIdx.x & 31, w = (blockIdx.x * kQoThreads + threadIdx.x) >> 5;
     pdl_trigger();
     pdl_wait();
-    if (w >= 2 * n_slabs) {                                   // the step's queries into their slot of the window
-        const int i = (w - 2 * n_slabs) * 32 + lane;
+    if (w >= 2 * kParts * n_slabs) {                          // the step's queries into their slot of the window
+        const int i = (w - 2 * kParts * n_slabs) * 32 + lane;
         if (a.q_win != nullptr && i < batch * a.Hq * 16) a.q_win[(size_t(i >> 4) * a.window + a.slot) * 16 + (i & 15)] = a.q[i];
         return;
     }
-    const int s = w >> 1, b = s / Hk, block = 1 << c.block_log2;
+    const int s = w / (2 * kParts), part = (w >> 1) & (kParts - 1), b = s / Hk, block = 1 << c.block_log2;
     const int lo = a.new_off ? a.new_off[b] : b, hi = a.new_off ? a.new_off[b + 1] : b + 1;
     const int row0 = c.table ? 0 : q8_row0(slab_off, cap, Hk, s);        // (read beside the length)
     const int old = a.len_in[s], room = q8_room(c, cap, Hk, s);
@@ -289,8 +338,14 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
     for (int done = 0; done < count;) {
         const int tok = old + done, j = tok / kQ8Tile, r = tok % kQ8Tile;
         const int held = r & (block - 1), take = min(count - done, block - held);        // rows that the block has, and that it gets
+        if (kParts > 1 && ((tok >> c.block_log2) & (kParts - 1)) != part) { done += take; continue; }
         const uint2* const x = src + done * next;
-        const uint2 x0 = *x;
+        uint2 y[kQoRows];
+        auto load = [&](int k0) {
+#pragma unroll
+            for (int i = 0; i < kQoRows; ++i) y[i] = k0 + i < take ? x[(k0 + i) * next] : make_uint2(0u, 0u);
+        };
+        load(0);
         done += take;
         const Q8Tile at = q8_tile(c, s, j, r + take, row0);
         if (at.row < 0) {
@@ -300,9 +355,13 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
         float* const scale = ((w & 1) ? c.v_scale : c.k_scale) + at.scale + (r >> c.block_log2);
         uint32_t* const row = reinterpret_cast<uint32_t*>(((w & 1) ? c.V : c.K) + (at.row + r) * kQ8RowBytes) + lane;
         const float s_old = held ? *scale : 0.f;
-        uint32_t m = __vmaxu2(x0.x & 0x7fff7fffu, x0.y & 0x7fff7fffu);
-#pragma unroll 4
-        for (int k = 1; k < take; ++k) m = __vimax3_u16x2(m, x[k * next].x & 0x7fff7fffu, x[k * next].y & 0x7fff7fffu);
+        uint32_t m = 0;
+#pragma unroll 1
+        for (int k0 = 0; k0 < take; k0 += kQoRows) {
+            if (k0) load(k0);
+#pragma unroll
+            for (int i = 0; i < kQoRows; ++i) m = __vimax3_u16x2(m, y[i].x & 0x7fff7fffu, y[i].y & 0x7fff7fffu);
+        }
         m = __reduce_max_sync(0xffffffffu, max(m & 0xffffu, m >> 16));
         const bool wild = m >= 0x7f80u;
         if (wild) {                                           // infinities and NaN do not count for the scale
@@ -314,29 +373,39 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
         int e = scale_exp<kFmt>(m);
         if (held) e = max(e, held_exp(s_old));                // a scale only grows
         const float s_new = pow2f(e), inv = pow2f(-e);
-#pragma unroll 4
-        for (int k = 0; k < take; ++k) {
-            uint2 y = k ? x[k * next] : x0;
-            if (wild) { uint32_t fin = 0; y.x = without_nan(y.x, fin); y.y = without_nan(y.y, fin); }
-            float2 v0 = bf16x2_to_f2(y.x), v1 = bf16x2_to_f2(y.y);
-            if (kFmt == SKIPKV_Q8_INT8 && wild) { v0 = within(v0, 127.f * s_new); v1 = within(v1, 127.f * s_new); }
-            row[k * (kQ8RowBytes / 4)] = kFmt == SKIPKV_Q8_INT8 ? q8_round_scaled(v0, v1, make_float2(inv, inv))
-                                                               : q8_round<kFmt>(v0.x * inv, v0.y * inv, v1.x * inv, v1.y * inv);
+#pragma unroll 1
+        for (int k0 = 0; k0 < take; k0 += kQoRows) {
+            if (take > kQoRows) load(k0);
+#pragma unroll
+            for (int i = 0; i < kQoRows; ++i) {
+                if (k0 + i >= take) break;
+                if (wild) { uint32_t fin = 0; y[i].x = without_nan(y[i].x, fin); y[i].y = without_nan(y[i].y, fin); }
+                float2 v0 = bf16x2_to_f2(y[i].x), v1 = bf16x2_to_f2(y[i].y);
+                if (kFmt == SKIPKV_Q8_INT8 && wild) { v0 = within(v0, 127.f * s_new); v1 = within(v1, 127.f * s_new); }
+                row[(k0 + i) * (kQ8RowBytes / 4)] = kFmt == SKIPKV_Q8_INT8 ? q8_round_scaled(v0, v1, make_float2(inv, inv))
+                                                                          : q8_round<kFmt>(v0.x * inv, v0.y * inv, v1.x * inv, v1.y * inv);
+            }
         }
         if (s_new == s_old) continue;
         __syncwarp();                                         // (every lane has read the scale)
         if (lane == 0) *scale = s_new;
         const float again = s_old * inv;                      // the rows that the block had, under the new scale
-#pragma unroll 4
-        for (int k = 1; k <= held; ++k) {
-            uint32_t* const p = row - k * (kQ8RowBytes / 4);
-            uint32_t f0, f1;
-            q8_to_f16<kFmt>(*p, f0, f1);
-            const float2 y0 = f16x2_to_f2(f0), y1 = f16x2_to_f2(f1);
-            *p = q8_round<kFmt>(y0.x * again, y0.y * again, y1.x * again, y1.y * again);
+#pragma unroll 1
+        for (int k0 = 1; k0 <= held; k0 += kQoHeld) {
+            uint32_t* const p = row - k0 * (kQ8RowBytes / 4);
+            uint32_t cd[kQoHeld];
+#pragma unroll
+            for (int i = 0; i < kQoHeld; ++i) cd[i] = k0 + i <= held ? p[-i * (kQ8RowBytes / 4)] : 0u;
+#pragma unroll
+            for (int i = 0; i < kQoHeld; ++i) {
+                uint32_t f0, f1;
+                q8_to_f16<kFmt>(cd[i], f0, f1);
+                const float2 y0 = f16x2_to_f2(f0), y1 = f16x2_to_f2(f1);
+                if (k0 + i <= held) p[-i * (kQ8RowBytes / 4)] = q8_round<kFmt>(y0.x * again, y0.y * again, y1.x * again, y1.y * again);
+            }
         }
     }
-    if (w & 1) return;
+    if (w & (2 * kParts - 1)) return;
     // ---- the length, and the rest of a decode step
     const int now = old + count;
     if (lane == 0) a.len_out[s] = now;
@@ -387,28 +456,53 @@ __device__ __forceinline__ uint4 values8(const uint2& x, float sc) {
 }
 
 // Codes back to bf16: K and V of a tile in turn (one of them where the other has no destination).
-template <int kFmt>
+struct LoadSlabs {
+    struct Raw { int len, cap; int64_t off; };
+    Q8View c;
+    const int64_t* slab_off;
+    const int32_t *cap, *kv_len;
+    uint32_t* status;
+    int Hk;
+    __device__ __forceinline__ Raw load(int s) const { return {kv_len[s], cap[s / Hk], slab_off[s / Hk]}; }
+    __device__ __forceinline__ Span span(int s, const Raw& r) const {
+        const int room = min(q8_room(c, r.cap), r.cap);
+        return {0, min(max(r.len, 0), max(room, 0)), q8_row0(r.off, r.cap, Hk, s), r.len < 0 || r.len > room};
+    }
+    __device__ __forceinline__ int count(int s, const Raw& r) const {
+        const Span x = span(s, r);
+        if (x.bad) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+        return (x.now + kQ8Tile - 1) / kQ8Tile;
+    }
+};
+
+template <int kFmt, bool kTable>
 __global__ void __launch_bounds__(kQsThreads, 6)
-q8_load_kernel(int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, Q8View c, const int32_t* kv_len, uint4* K, uint4* V,
-               long long dst_rows, uint32_t* status) {
+q8_load_kernel(int n_slabs, LoadSlabs slabs, uint4* K, uint4* V, long long dst_rows, const int* slab_table) {
     extern __shared__ __align__(16) uint8_t qsm[];
     int* pref = reinterpret_cast<int*>(qsm);
-    int* lens = pref + n_slabs + 1;
-    int* row0 = lens + n_slabs;                               // first rows in a contiguous layout
+    int* lens = pref + n_slabs + 1;                           // (not kTable)
+    int* row0 = lens + n_slabs;                               // (not kTable) first rows in a contiguous layout
+    const Q8View& c = slabs.c;
+    uint32_t* const status = slabs.status;
     __shared__ uint32_t s_wsum[kQsWarps];
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const int G = gridDim.x, cta = blockIdx.x;
     pdl_trigger();
     pdl_wait();
-    for (int s = tid; s < n_slabs; s += kQsThreads) {
-        row0[s] = q8_row0(slab_off, cap, Hk, s);
-        const int n = kv_len[s], room = min(q8_room(c, cap, Hk, s), cap[s / Hk]);
-        const bool bad = n < 0 || n > room;
-        if (bad && cta == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
-        lens[s] = min(max(n, 0), max(room, 0));
+    if (kTable) {
+#pragma unroll 4
+        for (int s = tid; s <= n_slabs; s += kQsThreads) pref[s] = slab_table[s];
+        __syncthreads();
+    } else {
+        for (int s = tid; s < n_slabs; s += kQsThreads) {
+            const Span x = slabs.span(s, slabs.load(s));
+            if (x.bad && cta == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
+            row0[s] = x.row0;
+            lens[s] = x.now;
+        }
+        __syncthreads();
+        cta_prefix<kQsThreads>(n_slabs, [&](int s) { return (lens[s] + kQ8Tile - 1) / kQ8Tile; }, pref, s_wsum);
     }
-    __syncthreads();
-    cta_prefix<kQsThreads>(n_slabs, [&](int s) { return (lens[s] + kQ8Tile - 1) / kQ8Tile; }, pref, s_wsum);
     const int per = (K ? 1 : 0) + (V ? 1 : 0);
     const Share share(pref[n_slabs] * per, cta, G);
     const int c16 = lane & 15, r0 = warp * 16 + (lane >> 4);
@@ -417,10 +511,11 @@ q8_load_kernel(int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap,
         const int t = per == 2 ? t2 >> 1 : t2;
         const bool is_v = per == 2 ? (t2 & 1) != 0 : V != nullptr;
         s = slab_of(pref, n_slabs, t, s);
-        const int j = t - pref[s], rows = min(lens[s] - j * kQ8Tile, kQ8Tile);
-        const Q8Tile at = q8_tile(c, s, j, rows, row0[s]);
-        const long long to = (long long)row0[s] + (long long)j * kQ8Tile;
-        if (at.row < 0 || row0[s] < 0 || to + rows > dst_rows) {
+        const Span x_s = kTable ? slabs.span(s, slabs.load(s)) : Span{0, lens[s], row0[s], false};
+        const int j = t - pref[s], rows = min(x_s.now - j * kQ8Tile, kQ8Tile);
+        const Q8Tile at = q8_tile(c, s, j, rows, x_s.row0);
+        const long long to = (long long)x_s.row0 + (long long)j * kQ8Tile;
+        if (at.row < 0 || x_s.row0 < 0 || to + rows > dst_rows) {
             if (tid == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
             continue;
         }
@@ -443,7 +538,7 @@ q8_load_kernel(int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap,
     }
 }
 
-int check_q8(const skipkv_q8_cache* c) {
+int check_q8(const skipkv_shape* s, const skipkv_q8_cache* c) {
     if (!c || !c->K || !c->V || !c->k_scale || !c->v_scale || c->rows <= 0) return SKIPKV_ERR_INVALID_ARG;
     if (c->format != SKIPKV_Q8_E4M3 && c->format != SKIPKV_Q8_INT8) return SKIPKV_ERR_UNSUPPORTED;
     if (c->block_rows != 16 && c->block_rows != 32 && c->block_rows != 64 && c->block_rows != 128) return SKIPKV_ERR_UNSUPPORTED;
@@ -451,6 +546,13 @@ int check_q8(const skipkv_q8_cache* c) {
     if ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 3) return SKIPKV_ERR_INVALID_ARG;
     if (c->block_table ? c->max_pages <= 0 || c->rows % kQ8Tile != 0 : c->max_blocks <= 0) return SKIPKV_ERR_INVALID_ARG;
     if (c->rows > int64_t(0x7fffffff) - 256) return SKIPKV_ERR_UNSUPPORTED;
+    const int64_t slabs = int64_t(s->batch) * s->n_kv_heads;
+    if (slabs > kQ8MaxSlabs) {
+        set_error_text("8-bit cache: batch * n_kv_heads above 8192");
+        return SKIPKV_ERR_UNSUPPORTED;
+    }
+    // places of scales, and tiles of K and V of all slabs, in 32 bits
+    if (slabs * (c->block_table ? c->max_pages : c->max_blocks) >= 1 << 30) return SKIPKV_ERR_UNSUPPORTED;
     if (c->device >= 0) {
         int dev = 0;
         SKIPKV_CUDA(cudaGetDevice(&dev));
@@ -466,11 +568,6 @@ int check_q8(const skipkv_q8_cache* c) {
 
 using namespace skipkv;
 
-static int too_many_slabs() {
-    set_error_text("8-bit cache: batch * n_kv_heads above 8192");
-    return SKIPKV_ERR_UNSUPPORTED;
-}
-
 // CTAs of a launch over at most `tiles` tiles: four (six) to an SM.
 static int store_grid(long long tiles, int per_sm) {
     const long long most = (long long)num_sms() * per_sm;
@@ -479,12 +576,24 @@ static int store_grid(long long tiles, int per_sm) {
 
 template <bool kAppend>
 static int store(const skipkv_shape* shape, const skipkv_q8_cache* cache, const StoreArgs& a, long long tiles, void* ws, void* stream) {
-    const int slabs = shape->batch * shape->n_kv_heads;
-    if (slabs > kQ8MaxSlabs) return too_many_slabs();
-    const size_t smem = (size_t(slabs) + 2) / 2 * 8 + size_t(slabs) * 12;
-    SKIPKV_CUDA(launch_dependent(cache->format == SKIPKV_Q8_E4M3 ? q8_store_kernel<SKIPKV_Q8_E4M3, kAppend> : q8_store_kernel<SKIPKV_Q8_INT8, kAppend>,
-                                 dim3(store_grid(2 * tiles, 4)), dim3(kQsThreads), smem, static_cast<cudaStream_t>(stream), int(shape->batch),
-                                 int(shape->n_kv_heads), slabs, shape->slab_off, shape->cap, q8_view(*cache), a, &static_cast<Header*>(ws)->status));
+    const int n_slabs = shape->batch * shape->n_kv_heads;
+    const bool table = n_slabs >= kQsTableSlabs;
+    uint8_t* w = static_cast<uint8_t*>(ws);
+    int* slab_table = reinterpret_cast<int*>(w + make_layout(*shape).slab_table);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const StoreSlabs<kAppend> slabs{q8_view(*cache), shape->slab_off, shape->cap, a.new_off, a.len_in, a.len_out, &static_cast<Header*>(ws)->status,
+                                    a.n_new, int(shape->n_kv_heads)};
+    if (table) SKIPKV_CUDA(launch_dependent(q8_table_kernel<StoreSlabs<kAppend>>, dim3(1), dim3(kQ8TableThreads), 0, st, n_slabs, slabs, slab_table));
+    const size_t prefix = (size_t(n_slabs) + 2) / 2 * 8, smem = table ? prefix : prefix + size_t(n_slabs) * 12;
+    auto run = [&](auto kernel) {
+        return launch_dependent(kernel, dim3(store_grid(2 * tiles, 4)), dim3(kQsThreads), smem, st, n_slabs, slabs, a,
+                                static_cast<const int*>(slab_table));
+    };
+    auto pick = [&](auto fmt) {
+        constexpr int kFmt = decltype(fmt)::value;
+        return table ? run(q8_store_kernel<kFmt, kAppend, true>) : run(q8_store_kernel<kFmt, kAppend, false>);
+    };
+    SKIPKV_CUDA(cache->format == SKIPKV_Q8_E4M3 ? pick(std::integral_constant<int, SKIPKV_Q8_E4M3>()) : pick(std::integral_constant<int, SKIPKV_Q8_INT8>()));
     return SKIPKV_OK;
 }
 
@@ -497,22 +606,29 @@ static int append(const skipkv_shape* shape, const skipkv_q8_cache* cache, const
     a.k_src = static_cast<const uint4*>(k_new); a.v_src = static_cast<const uint4*>(v_new);
     a.new_off = new_off; a.n_new = n_new; a.len_in = kv_len_in; a.len_out = kv_len_out;
     const int slabs = shape->batch * shape->n_kv_heads;
-    if (new_off && n_new > shape->batch) {
+    if (new_off && (long long)n_new > (long long)kQoMost * shape->batch) {
         // a slab's new rows lie in one tile more than they fill, at most
         return store<true>(shape, cache, a, (long long)n_new * shape->n_kv_heads / kQ8Tile + 2ll * slabs, ws, stream);
     }
-    const long long warps = 2ll * slabs + (a.q_win ? ((long long)shape->batch * shape->n_q_heads * 16 + 31) / 32 : 0);
-    SKIPKV_CUDA(launch_dependent(cache->format == SKIPKV_Q8_E4M3 ? q8_append_few_kernel<SKIPKV_Q8_E4M3> : q8_append_few_kernel<SKIPKV_Q8_INT8>,
-                                 dim3(unsigned((warps * 32 + kQoThreads - 1) / kQoThreads)), dim3(kQoThreads), 0, static_cast<cudaStream_t>(stream),
-                                 int(shape->batch), int(shape->n_kv_heads), slabs, shape->slab_off, shape->cap, q8_view(*cache), a,
-                                 &static_cast<Header*>(ws)->status));
+    const bool parts = n_new > shape->batch;
+    const long long warps = (parts ? 2ll * kQoParts : 2ll) * slabs + (a.q_win ? ((long long)shape->batch * shape->n_q_heads * 16 + 31) / 32 : 0);
+    auto run = [&](auto kernel) {
+        return launch_dependent(kernel, dim3(unsigned((warps * 32 + kQoThreads - 1) / kQoThreads)), dim3(kQoThreads), 0, static_cast<cudaStream_t>(stream),
+                                int(shape->batch), int(shape->n_kv_heads), slabs, shape->slab_off, shape->cap, q8_view(*cache), a,
+                                &static_cast<Header*>(ws)->status);
+    };
+    auto pick = [&](auto fmt) {
+        constexpr int kFmt = decltype(fmt)::value;
+        return parts ? run(q8_append_few_kernel<kFmt, kQoParts>) : run(q8_append_few_kernel<kFmt, 1>);
+    };
+    SKIPKV_CUDA(cache->format == SKIPKV_Q8_E4M3 ? pick(std::integral_constant<int, SKIPKV_Q8_E4M3>()) : pick(std::integral_constant<int, SKIPKV_Q8_INT8>()));
     return SKIPKV_OK;
 }
 
 extern "C" int skipkv_pack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* K, const void* V,
                               const int32_t* kv_len, void* ws, void* stream) {
     if (int rc = check_shape(shape)) return rc;
-    if (int rc = check_q8(cache)) return rc;
+    if (int rc = check_q8(shape, cache)) return rc;
     if (!K || !V || !kv_len) return SKIPKV_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15) return SKIPKV_ERR_INVALID_ARG;
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return SKIPKV_ERR_WORKSPACE;
@@ -527,7 +643,7 @@ extern "C" int skipkv_append_q8(const skipkv_shape* shape, const skipkv_q8_cache
                                 const int32_t* new_off, int32_t n_new, const int32_t* kv_len_in, int32_t* kv_len_out, void* ws,
                                 void* stream) {
     if (int rc = check_shape(shape)) return rc;
-    if (int rc = check_q8(cache)) return rc;
+    if (int rc = check_q8(shape, cache)) return rc;
     return append(shape, cache, k_new, v_new, new_off, n_new, kv_len_in, kv_len_out, StoreArgs{}, ws, stream);
 }
 
@@ -536,7 +652,7 @@ extern "C" int skipkv_append_step_q8(const skipkv_shape* shape, const skipkv_q8_
                                      int32_t* n_sent, const uint8_t* new_sent, const int32_t* gen_id, void* q_win, const void* q,
                                      int32_t slot, void* ws, void* stream) {
     if (int rc = check_shape(shape)) return rc;
-    if (int rc = check_q8(cache)) return rc;
+    if (int rc = check_q8(shape, cache)) return rc;
     if (!sent_off || !sent_id || !n_sent || !new_sent || !gen_id || shape->max_sent <= 0) return SKIPKV_ERR_INVALID_ARG;
     if ((q_win != nullptr) != (q != nullptr)) return SKIPKV_ERR_INVALID_ARG;
     if (q_win && (slot < 0 || slot >= shape->window)) return SKIPKV_ERR_INVALID_ARG;
@@ -551,16 +667,26 @@ extern "C" int skipkv_append_step_q8(const skipkv_shape* shape, const skipkv_q8_
 extern "C" int skipkv_unpack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const int32_t* kv_len, void* K, void* V,
                                 void* ws, void* stream) {
     if (int rc = check_shape(shape)) return rc;
-    if (int rc = check_q8(cache)) return rc;
+    if (int rc = check_q8(shape, cache)) return rc;
     if (!kv_len || (!K && !V)) return SKIPKV_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(K) | reinterpret_cast<uintptr_t>(V)) & 15) return SKIPKV_ERR_INVALID_ARG;
     if (!ws || (reinterpret_cast<uintptr_t>(ws) & 255)) return SKIPKV_ERR_WORKSPACE;
-    const int slabs = shape->batch * shape->n_kv_heads;
-    if (slabs > kQ8MaxSlabs) return too_many_slabs();
-    const long long tiles = (long long)slabs * ((shape->max_cap + kQ8Tile - 1) / kQ8Tile) * ((K ? 1 : 0) + (V ? 1 : 0));
-    SKIPKV_CUDA(launch_dependent(cache->format == SKIPKV_Q8_E4M3 ? q8_load_kernel<SKIPKV_Q8_E4M3> : q8_load_kernel<SKIPKV_Q8_INT8>,
-                                 dim3(store_grid(tiles, 6)), dim3(kQsThreads), size_t(3 * slabs + 1) * 4, static_cast<cudaStream_t>(stream),
-                                 int(shape->n_kv_heads), slabs, shape->slab_off, shape->cap, q8_view(*cache), kv_len, static_cast<uint4*>(K),
-                                 static_cast<uint4*>(V), static_cast<long long>(shape->total_rows), &static_cast<Header*>(ws)->status));
+    const int n_slabs = shape->batch * shape->n_kv_heads;
+    const long long tiles = (long long)n_slabs * ((shape->max_cap + kQ8Tile - 1) / kQ8Tile) * ((K ? 1 : 0) + (V ? 1 : 0));
+    const bool table = n_slabs >= kQsTableSlabs;
+    int* slab_table = reinterpret_cast<int*>(static_cast<uint8_t*>(ws) + make_layout(*shape).slab_table);
+    cudaStream_t st = static_cast<cudaStream_t>(stream);
+    const LoadSlabs slabs{q8_view(*cache), shape->slab_off, shape->cap, kv_len, &static_cast<Header*>(ws)->status, int(shape->n_kv_heads)};
+    if (table) SKIPKV_CUDA(launch_dependent(q8_table_kernel<LoadSlabs>, dim3(1), dim3(kQ8TableThreads), 0, st, n_slabs, slabs, slab_table));
+    auto run = [&](auto kernel) {
+        return launch_dependent(kernel, dim3(store_grid(tiles, 6)), dim3(kQsThreads), size_t(table ? n_slabs + 1 : 3 * n_slabs + 1) * 4, st, n_slabs,
+                                slabs, static_cast<uint4*>(K), static_cast<uint4*>(V), static_cast<long long>(shape->total_rows),
+                                static_cast<const int*>(slab_table));
+    };
+    auto pick = [&](auto fmt) {
+        constexpr int kFmt = decltype(fmt)::value;
+        return table ? run(q8_load_kernel<kFmt, true>) : run(q8_load_kernel<kFmt, false>);
+    };
+    SKIPKV_CUDA(cache->format == SKIPKV_Q8_E4M3 ? pick(std::integral_constant<int, SKIPKV_Q8_E4M3>()) : pick(std::integral_constant<int, SKIPKV_Q8_INT8>()));
     return SKIPKV_OK;
 }

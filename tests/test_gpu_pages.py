@@ -355,3 +355,15 @@ def test_server_loop(B, fmt, block):
     check()
     sv.ask(np.zeros(bt * hk))
     assert sv.free == pool
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two devices")
+def test_tensors_of_another_device_are_refused(B):
+    here, there = (torch.zeros(1, 1, dtype=torch.int32, device=f"cuda:{i}") for i in (0, 1))
+    slots = torch.zeros(1, 1, dtype=torch.int64, device="cuda:0")
+    with torch.cuda.device(0):
+        for k in range(3):
+            a = [here] * 3
+            a[k] = there
+            with pytest.raises(ValueError, match="another device"):
+                B.skipkv_slot_map(1, 1, 1, *a, None, 1, slots)

@@ -102,6 +102,19 @@ def test_attention_over_more_slabs_than_blocks(B):
     check_attention(c, q, attend(c, q))
 
 
+@pytest.mark.parametrize("paged", [False, True])
+def test_attention_where_few_of_many_slabs_have_rows(B, paged):
+    """A block's range goes from one slab over hundreds of empty ones to the next."""
+    lens = np.zeros((700, 2), np.int64)
+    for s, n in ((3, 20000), (4, 1), (5, 129), (300, 40000), (301, 700), (1000, 5), (1007, 128), (1398, 9000), (1399, 1)):
+        lens[s // 2, s % 2] = n
+    caps = np.maximum(lens.max(1), 1)
+    c = filled(B, lens, caps, 2, "e4m3", 64, paged, 2, n_q=4)
+    q = queries(c, 4, 6)
+    check_attention(c, q, attend(c, q))
+    assert c.status() == 0
+
+
 @pytest.mark.parametrize("fmt", FORMATS)
 @pytest.mark.parametrize("q_size,sigma", [(0.0, 1.0), (1e30, 1e-30), (1e-30, 1e30), (2e4, 2.0 ** -9), (1e-38, 1.0), (30.0, 1.0)])
 def test_attention_over_extreme_magnitudes(B, fmt, q_size, sigma):
@@ -426,6 +439,103 @@ def test_append_no_more_rows_than_sequences(B, fmt, paged, block):
         assert np.array_equal(b.cpu().numpy().reshape(-1), lens)
         a, b = b, a
     c.untouched(lens)
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("block", [16, 64, 128])
+def test_append_up_to_four_rows_per_sequence(B, fmt, paged, block):
+    """As many rows as a call may have whose slabs are shared out by blocks, and one more: equal parts, one sequence with all of them, scales that grow."""
+    hk, bt = 2, 21
+    c = Cache(B, np.zeros((bt, hk)), [400] * bt, hk, fmt, block, paged, 13)
+    host = [([np.zeros((400, 128), np.uint8) for _ in range(c.slabs)], [np.zeros(-(-400 // block)) for _ in range(c.slabs)]) for _ in range(2)]
+    lens = np.zeros(c.slabs, np.int32)
+    a, b = torch.zeros(bt, hk, dtype=torch.int32, device="cuda"), torch.full((bt, hk), -1, dtype=torch.int32, device="cuda")
+    parts = [[4] * 21, [84] + [0] * 20, [5] * 16 + [4, 0, 0, 0, 0], [61, 0, 3] + [1] * 18, [0] * 20 + [85], [1] * 20 + [64], [0, 22] + [0] * 19]
+    for i, part in enumerate(parts):
+        off = np.concatenate([[0], np.cumsum(part)])
+        x = [bf16(values(c.r, int(off[-1]) * hk, wild=i == 3).double().numpy().reshape(-1, hk, 128) * 2.0 ** (2 * i - 6)) for _ in range(2)]
+        B.skipkv_append_q8(c.shape, c.cache, x[0].cuda(), x[1].cuda(), torch.from_numpy(off.astype(np.int32)).cuda(), int(off[-1]), a, b, c.ws)
+        torch.cuda.synchronize()
+        assert c.status() == (8 if i == 3 else 0)
+        for s in range(c.slabs):
+            q, h = divmod(s, hk)
+            for k in range(2):
+                n = oracle.q8_append(host[k][0][s], host[k][1][s], int(lens[s]), x[k][int(off[q]):int(off[q + 1]), h].double().numpy(), block, fmt)
+            lens[s] = n
+            same(c, s, n, [host[0][0][s], host[1][0][s]], [host[0][1][s], host[1][1][s]])
+        assert np.array_equal(b.cpu().numpy().reshape(-1), lens)
+        a, b = b, a
+    c.untouched(lens)
+
+
+@pytest.mark.parametrize("paged", [False, True])
+def test_many_slabs_stored_appended_and_loaded(B, paged):
+    """So many slabs that their table has a launch of its own; most are empty.  The calls behind one another leave what they leave with a pause after each."""
+    hk, bt, block, fmt = 2, 1100, 16, "e4m3"
+    r = np.random.default_rng(5)
+    lens = np.where(r.random((bt, hk)) < 0.1, r.integers(0, 140, (bt, hk)), 0)
+    lens[-1] = 140
+    part = np.where(r.random(bt) < 0.3, r.integers(0, 30, bt), 0)
+    part[7] = 25
+    part[9] += max(0, 4 * bt + 1 - int(part.sum()))
+    room = int((lens.max(1) + part).max()) + 20
+    off = np.concatenate([[0], np.cumsum(part)]).astype(np.int32)
+    new = [values(r, int(off[-1]) * hk).view(-1, hk, 128) for _ in range(2)]
+    got = []
+    for pause in (True, False):
+        c = Cache(B, lens, [room] * bt, hk, fmt, block, paged, 2, n_q=2 * hk)
+        src = [torch.from_numpy(np.random.default_rng(8 + i).normal(0, 1, (c.rows16, 128)).astype(np.float32)).bfloat16().cuda() for i in range(2)]
+        n1, n2 = torch.full_like(c.kv_len, -1), torch.full_like(c.kv_len, -1)
+        dev, offs = [x.cuda() for x in new], torch.from_numpy(off).cuda()
+        out, back, q = torch.full((bt, 2 * hk, 128), 3.0, dtype=torch.bfloat16, device="cuda"), torch.full_like(src[0], 7.0), queries(c, 2 * hk, 3)
+        torch.cuda.synchronize()
+        calls = [lambda: B.skipkv_pack_q8(c.shape, c.cache, src[0], src[1], c.kv_len, c.ws),
+                 lambda: B.skipkv_append_q8(c.shape, c.cache, dev[0], dev[1], offs, int(off[-1]), c.kv_len, n1, c.ws),
+                 lambda: B.skipkv_decode_attn_q8(c.shape, c.cache, q, n1, out, None, None, None, None, c.ws),
+                 lambda: B.skipkv_append_q8(c.shape, c.cache, dev[0][:bt], dev[1][:bt], None, bt, n1, n2, c.ws),
+                 lambda: B.skipkv_unpack_q8(c.shape, c.cache, n2, None, back, c.ws)]
+        for f in calls:
+            f()
+            if pause:
+                torch.cuda.synchronize()
+        torch.cuda.synchronize()
+        assert c.status() == 0
+        got.append([out, back, n1, n2, c.K, c.V, c.ks.view(torch.int32), c.vs.view(torch.int32)])
+        if not pause:
+            break
+        host = [x.double().cpu().numpy() for x in src]
+        want_n1, want_n2 = lens + part[:, None], lens + part[:, None] + 1
+        assert np.array_equal(n1.cpu().numpy(), want_n1) and np.array_equal(n2.cpu().numpy(), want_n2)
+        V = back.double().cpu().numpy()
+        x64, live = [x.double().numpy() for x in new], np.zeros(c.rows16, bool)
+        c.rows64 = [[], []]
+        for s in range(c.slabs):
+            b, h = divmod(s, hk)
+            n = int(want_n2[b, h])
+            codes, scale = np.zeros((room, 128), np.uint8), np.zeros(-(-room // block))
+            end = []
+            for k in range(2):
+                old = int(lens[b, h])
+                oracle.q8_append(codes, scale, 0, host[k][c.row0[s]:c.row0[s] + old], block, fmt)
+                m = oracle.q8_append(codes, scale, old, x64[k][off[b]:off[b + 1], h], block, fmt)
+                c.rows64[k].append(oracle.q8_rows(codes, scale, m, block, fmt))
+                if k == 1:
+                    oracle.q8_append(codes, scale, m, x64[k][b:b + 1, h], block, fmt)
+                    assert np.array_equal(V[c.row0[s]:c.row0[s] + n], oracle.q8_rows(codes, scale, n, block, fmt)), s
+            live[c.row0[s]:c.row0[s] + n] = True
+        assert (V[~live] == 7).all()
+        check_attention(c, q, out)
+        # a length without room is reported, its slab left out
+        bad = c.kv_len.clone()
+        bad[3, 1] = room + 200
+        B.skipkv_pack_q8(c.shape, c.cache, src[0], src[1], bad, c.ws)
+        torch.cuda.synchronize()
+        assert c.status() == 4
+        c2 = got[0]
+        got[0] = [x.clone() for x in c2[:4]]
+    for x, y in zip(got[0], got[1]):
+        assert torch.equal(x, y)
 
 
 def test_append_where_heads_differ_in_length(B):

@@ -160,6 +160,20 @@ def test_bad_arguments_are_refused(binding):
     assert lib.skipkv_unpack_q8(C.byref(many), k, p, p, p, p, none) == -2
 
 
+@pytest.mark.parametrize("over", [dict(max_blocks=1 << 28), dict(block_table=256, max_pages=1 << 28)])
+def test_tables_beyond_32_bits_are_refused(binding, over):
+    """Four slabs: 2^30 scales or pages, whose places and tiles (K and V) would not be numbers of 32 bits."""
+    lib = binding.lib()
+    shape, c = _args(binding, **over)
+    s, k, p, none = C.byref(shape), C.byref(c), C.c_void_p(4096), C.c_void_p(None)
+    assert lib.skipkv_pack_q8(s, k, p, p, p, p, none) == -2
+    assert lib.skipkv_append_q8(s, k, p, p, p, 2, p, C.c_void_p(8192), p, none) == -2
+    assert lib.skipkv_decode_attn_q8(s, k, p, p, p, none, none, none, none, p, none) == -2
+    assert lib.skipkv_unpack_q8(s, k, p, p, p, p, none) == -2
+    # a range of tokens whose end and one pass of a warp more is no number of 32 bits
+    assert lib.skipkv_slot_map(1, 1, 4, p, p, p, p, (1 << 31) - 1, p, none) == -2
+
+
 def test_page_calls_refuse_bad_arguments(binding):
     lib = binding.lib()
     p, q, none = C.c_void_p(4096), C.c_void_p(8192), C.c_void_p(None)
