@@ -110,8 +110,8 @@ __device__ __forceinline__ uint32_t q8_round_scaled(float2 a, float2 b, float2 k
 }
 
 // Many slabs: one CTA, in a launch of its own, makes the prefix sum over the slabs' tiles that the CTAs of the launch behind it else make each for
-// itself, which takes the longer the more slabs there are, and shared memory that costs resident CTAs.  8192 slabs of 500 rows: attention 226 us
-// with it against 460, storing 531 against 1050, loading 580 against 694.
+// itself, which takes the longer the more slabs there are, and shared memory that costs resident CTAs.  8192 slabs of 500 rows: attention 217 us
+// with it against 460, storing 531 against 1050, loading 581 against 694.
 constexpr int kQ8TableThreads = 1024;
 constexpr int kQ8TableEach = kQ8MaxSlabs / kQ8TableThreads;
 
