@@ -268,8 +268,19 @@ def time_extras(cfg, B, flush, clean, peaks, reps=10):
     out["decode_attn_us"] = timed(lambda: D.decode_attn(steer=True))
     out["decode_attn_paged_us"] = timed(lambda: B.skipkv_decode_attn_paged(
         D.shape, D.q, Kp, Vp, table, max_pages, D.kv_len, D.out, D.hidden, D.steer_vec, D.alpha, D.flag, D.ws))
+    # the same rows kept in 8 bits: stored, attended to, brought back, and one token of each sequence appended
+    max_blocks = int(D.kv_len.max().item()) // 64 + 1
+    codes = [torch.empty(D.K.shape[0], 128, dtype=torch.float8_e4m3fn, device=dev) for _ in range(2)]
+    scales = [torch.empty(cfg.batch, cfg.n_kv_heads, max_blocks, device=dev) for _ in range(2)]
+    q8 = B.make_q8_cache(codes[0], codes[1], scales[0], scales[1], 64)
+    kv_next, one = torch.empty_like(D.kv_len), torch.randn(cfg.batch, cfg.n_kv_heads, 128, device=dev).bfloat16()
+    out["pack_q8_us"] = timed(lambda: B.skipkv_pack_q8(D.shape, q8, D.K, D.V, D.kv_len, D.ws))
+    out["decode_attn_q8_us"] = timed(lambda: B.skipkv_decode_attn_q8(D.shape, q8, D.q, D.kv_len, D.out, D.hidden, D.steer_vec, D.alpha,
+                                                                     D.flag, D.ws))
+    out["unpack_q8_us"] = timed(lambda: B.skipkv_unpack_q8(D.shape, q8, D.kv_len, D.K, D.V, D.ws))
+    out["append_q8_us"] = timed(lambda: B.skipkv_append_q8(D.shape, q8, one, one, None, cfg.batch, D.kv_len, kv_next, D.ws))
     D.status()
-    del Kp, Vp
+    del Kp, Vp, codes, scales, q8
     del D, pristine, tok_keep
     torch.cuda.empty_cache()
     # one decode step of the decode-loop workload (cache a little above its budget of 2048): two launches against one
@@ -377,7 +388,7 @@ def main():
     ap.add_argument("--no-e2e", action="store_true")
     ap.add_argument("--extras", action="store_true",
                     help="also time the entry points beside the main path (lookup table, exactly-B variants, "
-                         "token-level redundancy); reported under \"extras\", not part of `value`")
+                         "8-bit cache, token-level redundancy); reported under \"extras\", not part of `value`")
     args = ap.parse_args()
     args.warmup = max(args.warmup, 3) if args.impl == "skipkv" else args.warmup
 
