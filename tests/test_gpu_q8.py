@@ -103,6 +103,33 @@ def test_attention_over_more_slabs_than_blocks(B):
 
 
 @pytest.mark.parametrize("paged", [False, True])
+def test_many_slabs_replayed_with_other_lengths_and_steered(B, paged):
+    """The table of the slabs belongs to a call: a captured one makes it anew from the lengths that it finds."""
+    r = np.random.default_rng(3)
+    c = filled(B, r.integers(0, 260, (150, 8)), [260] * 150, 8, "int8", 32, paged, 2, n_q=40, d_model=64)
+    q, out = queries(c, 40, 6), torch.zeros(150, 40, 128, dtype=torch.bfloat16, device="cuda")
+    start, vec = bf16(r.normal(0, 1, (150, 64))).cuda(), bf16(r.normal(0, 1, 64)).cuda()
+    alpha, flag = torch.from_numpy(r.random(150).astype(np.float32)).cuda(), torch.from_numpy(r.integers(0, 2, 150).astype(np.uint8)).cuda()
+    want, hidden = start.clone(), start.clone()
+    B.skipkv_steer(150, 64, want, vec, alpha, flag)
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        B.skipkv_decode_attn_q8(c.shape, c.cache, q, c.kv_len, out, hidden, vec, alpha, flag, c.ws)
+    full = c.kv_len.clone()
+    for lens in (full, torch.zeros_like(full), full // 2, full * (torch.arange(1200, device="cuda").view(150, 8) % 97 == 0).int()):
+        c.kv_len.copy_(lens)
+        out.fill_(float("nan"))
+        hidden.copy_(start)
+        g.replay()
+        torch.cuda.synchronize()
+        assert c.status() == 0 and torch.equal(hidden, want) and torch.equal(out, attend(c, q))
+        n = lens.view(-1).tolist()
+        d, c.rows64 = c.rows64, [[x[:k] for x, k in zip(y, n)] for y in c.rows64]
+        check_attention(c, q, out, only=range(0, 1200, 97))
+        c.rows64 = d
+
+
+@pytest.mark.parametrize("paged", [False, True])
 def test_attention_where_few_of_many_slabs_have_rows(B, paged):
     """A block's range goes from one slab over hundreds of empty ones to the next."""
     lens = np.zeros((700, 2), np.int64)
