@@ -20,8 +20,8 @@
 //    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates).  Up to four heads per group the eight columns hold the
 //    high and low parts of a head side by side, so that a lane has one head to exponentiate.
 //  * An arrival's answer is not waited for before the CTA's next part; the partials of a slab come to its last CTA through shared memory, 16 at a time.
-// What it takes (back to back, and what bounds it): one sequence of 2048 tokens 8.0 us, latency (wait 0.9, first rows 2.4, a tile 1.5, arrival 1.0,
-// merge 1.7); 80 slabs of 4.1K 19.4 us, 0.66 of the copy rate: head and tail of a launch, between them 7.5 TB/s into the SMs; 128 slabs of 8.2K
+// What it takes (back to back, and what bounds it): one sequence of 2048 tokens 7.8 us, latency (wait 0.9, first rows 2.0, a tile 0.9, its warps
+// merged 0.6, arrival 0.9, merge 1.7); 80 slabs of 4.1K 19.4 us, 0.66 of the copy rate: head and tail of a launch, between them 7.5 TB/s into the SMs; 128 slabs of 8.2K
 // behind pages, int8, five heads 50.2 us, 0.81: conversions and latency; 128 slabs of 32K to 64K 240 us, 1.02, and 280 in seconds of it (power).
 #include <type_traits>
 
@@ -83,6 +83,18 @@ __device__ __forceinline__ void split_f16(float2 x, uint32_t& hi, uint32_t& lo) 
     hi = pack_f16(x.x, x.y);
     const float2 r = __ffma2_rn(f16x2_to_f2(hi), make_float2(-1.f, -1.f), x);
     lo = pack_f16(r.x, r.y);
+}
+// Four f16 values to e4m3; 32 (y - h) of two f16 values
+__device__ __forceinline__ uint32_t f16_to_e4m3(uint32_t a, uint32_t b) {
+    uint32_t r;
+    asm("{\n\t.reg .b16 x, y;\n\tcvt.rn.satfinite.e4m3x2.f16x2 x, %1;\n\tcvt.rn.satfinite.e4m3x2.f16x2 y, %2;\n\tmov.b32 %0, {x, y};\n\t}" : "=r"(r) : "r"(a), "r"(b));
+    return r;
+}
+__device__ __forceinline__ uint32_t rest32(uint32_t y, uint32_t h) {
+    uint32_t d;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(d) : "r"(y), "r"(h));
+    asm("mul.rn.f16x2 %0, %0, %1;" : "+r"(d) : "r"(0x50005000u));
+    return d;
 }
 __device__ __forceinline__ uint4 lds128(uint32_t addr) {
     uint4 r;
@@ -204,8 +216,6 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             asm volatile("prefetch.global.L2 [%0];" ::"l"(((tid & 1) ? c.v_scale : c.k_scale) + at));
         }
     }
-    if (!kTable) pdl_wait();
-
     // ---- copies: this warp's 32 rows of the CTA's k-th tile, and their scales, go to stage k % kQdStages.  The cursor walks the slab parts of
     // the range; divisions and the slab's tables are read once per part, a page's entry a tile ahead, and whole tiles take a short path.
     const uint32_t ring = smem_u32(dsm) + warp * kQdStages * kQdStageBytes;
@@ -235,6 +245,30 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
         }
         if (lane < 4) cp_async4(sp_dst + p_stage * 16, scale);
     };
+    // the next slab part; false: there is none
+    auto enter = [&]() {
+        if (pref[p_slab + 1] <= p_t) p_slab = slab_at(p_slab, p_t);
+        p_end = pref[p_slab + 1];
+        p_t = max(p_t, pref[p_slab] + kQdPartCost);
+        if (p_t >= t_end) { p_t = p_end = t_end; return false; }
+        if (c.table) {
+            p_table = c.table + size_t(p_slab) * c.max_pages + (p_t - pref[p_slab] - kQdPartCost);
+            p_page = p_t == t_begin ? int(row_first) : __ldcg(p_table);
+        } else {
+            const long long row0 = p_t == t_begin ? row_first : slab_row(p_slab);
+            p_row0 = int(row0 < 0 || row0 > c.rows ? c.rows : row0);
+        }
+        return true;
+    };
+    // the whole tiles from the slab's tile j = that at p_t on
+    auto whole_tiles = [&](int j) {
+        const int whole = lens[p_slab] / kQ8Tile;
+        p_fast = !c.table && (long long)p_row0 + (long long)whole * kQ8Tile > c.rows ? 0 : min(min(p_end, t_end) - p_t, whole - j);
+        if (!c.table) {
+            p_off = size_t(uint32_t(p_row0)) * kQ8RowBytes + size_t(j) * (kQ8Tile * kQ8RowBytes) + lane_off;
+            p_sp = sp + p_slab * c.max_blocks + j * per_tile + sub;
+        }
+    };
     // early: under the schedule from before the wait, with a length that may be old: all of the tile is copied
     auto issue_next = [&](bool early) {
         bool fast = p_fast > 0;
@@ -253,20 +287,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             ++p_t;
             if (++p_stage == kQdStages) p_stage = 0;
         } else if (p_t < t_end) {
-            if (p_t == p_end) {
-                if (pref[p_slab + 1] <= p_t) p_slab = slab_at(p_slab, p_t);
-                p_end = pref[p_slab + 1];
-                p_t = max(p_t, pref[p_slab] + kQdPartCost);
-                if (p_t >= t_end) { p_t = p_end = t_end; cp_async_commit(); return; }
-                const int j = p_t - pref[p_slab] - kQdPartCost;
-                if (c.table) {
-                    p_table = c.table + size_t(p_slab) * c.max_pages + j;
-                    p_page = p_t == t_begin ? int(row_first) : __ldcg(p_table);
-                } else {
-                    const long long row0 = p_t == t_begin ? row_first : slab_row(p_slab);
-                    p_row0 = int(row0 < 0 || row0 > c.rows ? c.rows : row0);
-                }
-            }
+            if (p_t == p_end && !enter()) { cp_async_commit(); return; }
             const int j = p_t - pref[p_slab] - kQdPartCost, left = lens[p_slab] - j * kQ8Tile, p_rows = left - warp * kQdRows;
             // (a page outside the pool: a row at which nothing lies; this warp's first row, at most the buffer's end)
             const int row = c.table ? (uint32_t(p_page) < uint32_t(pages) ? p_page * kQ8Tile + warp * kQdRows : int(c.rows))
@@ -297,19 +318,12 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                 far = far || (early && !in);
                 if (lane == 0 && rows > 0 && !early) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
             }
-            // the whole tiles behind it
-            const int whole = lens[p_slab] / kQ8Tile;
-            p_fast = !c.table && (long long)p_row0 + (long long)whole * kQ8Tile > c.rows ? 0 : min(min(p_end, t_end) - p_t, whole - j) - 1;
-            if (!c.table) {
-                p_off = size_t(uint32_t(p_row0)) * kQ8RowBytes + size_t(j + 1) * (kQ8Tile * kQ8RowBytes) + lane_off;
-                p_sp = sp + place + per_tile;
-            }
             ++p_t;
+            whole_tiles(j + 1);
             if (++p_stage == kQdStages) p_stage = 0;
         }
         cp_async_commit();                                // empty groups keep the count
     };
-    // What else comes from memory before the first tile is requested here and consumed behind the first copies.
     const int g = lane >> 2, qd = lane & 3;               // mma fragments: rows (tokens, channels) g and g + 8, columns (heads) 2 qd and 2 qd + 1
     // Few heads: columns 2 h and 2 h + 1 belong to head h (high and low parts), so a lane has one head, qd; else column h to head h.
     const int hd = kFew ? g >> 1 : g;                     // head of this lane's column of the B operands
@@ -322,19 +336,28 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             qa[4 * i] = v.x; qa[4 * i + 1] = v.y; qa[4 * i + 2] = v.z; qa[4 * i + 3] = v.w;
         }
     };
+    // The first copies' addresses are made ahead of the wait; what else comes from memory before the first tile is requested behind the first copies and
+    // waited for behind the second ones.
     int q_slab = slab;
+    if (t_begin < t_end && enter()) whole_tiles(p_t - pref[p_slab] - kQdPartCost);
+    if (!kTable) pdl_wait();
+    issue_next(!kTable);
     if (t_begin < t_end) fetch_q(slab);
-    const int len_again = !kTable && s_lo < s_hi ? length(s_lo) : 0;
-    const long long row_again = kTable ? 0 : first_row();
+    // the same for what the schedule was made of (as it comes: what is made of it waits for it)
+    const bool mine = !kTable && s_lo < s_hi, work = !kTable && t_begin < t_end;
+    const int len_again = mine ? __ldcg(kv_len + s_lo) : 0, room_again = mine ? __ldcg(cap + s_lo / Hk) : 0;
+    const int page_again = work && c.table ? __ldcg(c.table + size_t(slab) * c.max_pages + (t_begin - pref[slab] - kQdPartCost)) : 0;
+    const long long off_again = work && !c.table ? __ldcg(reinterpret_cast<const long long*>(slab_off) + slab / Hk) : 0;
+    const int cap_again = work && !c.table ? __ldcg(cap + slab / Hk) : 0;
 #pragma unroll 1
     for (int attempt = kTable ? 1 : 0;; ++attempt) {
 #pragma unroll 1
-        for (int k = 0; k < kQdStages - 1; ++k) issue_next(attempt == 0);
+        for (int k = kTable || attempt == 0; k < kQdStages - 1; ++k) issue_next(attempt == 0);
         if (attempt) break;
-        int changed = row_again != row_first || far;
+        int changed = far || (work && row_first != (c.table ? (long long)page_again : off_again * Hk + (long long)(slab % Hk) * cap_again));
 #pragma unroll 1
         for (int s = s_lo; s < s_hi; ++s) {
-            const int now = s == s_lo ? len_again : length(s);
+            const int now = s == s_lo ? min(max(len_again, 0), q8_room(c, room_again)) : length(s);
             if (now == lens[s]) continue;
             // (a slab that now reaches beyond the buffer is left to the checks of the second attempt)
             if (tiles(now) != tiles(lens[s]) || (!c.table && (long long)slab_row0(slab_off, cap, Hk, s / Hk, s % Hk) + now > c.rows)) changed = 1;
@@ -378,13 +401,12 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
         if (kFmt == SKIPKV_Q8_E4M3) {
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
+                // (as f16 the values have the bits that the two parts take)
                 const float2 v0 = bf16x2_to_f2(qa[2 * i]), v1 = bf16x2_to_f2(qa[2 * i + 1]);
-                const float y[4] = {v0.x * up, v0.y * up, v1.x * up, v1.y * up};
-                const uint32_t hi = q8_round<SKIPKV_Q8_E4M3>(y[0], y[1], y[2], y[3]);
+                const uint32_t y0 = pack_f16(v0.x * up, v0.y * up), y1 = pack_f16(v1.x * up, v1.y * up), hi = f16_to_e4m3(y0, y1);
                 uint32_t h0, h1;
                 q8_to_f16<SKIPKV_Q8_E4M3>(hi, h0, h1);
-                const float2 f0 = f16x2_to_f2(h0), f1 = f16x2_to_f2(h1);
-                const uint32_t lo = q8_round<SKIPKV_Q8_E4M3>((y[0] - f0.x) * 32.f, (y[1] - f0.y) * 32.f, (y[2] - f1.x) * 32.f, (y[3] - f1.y) * 32.f);
+                const uint32_t lo = f16_to_e4m3(rest32(y0, h0), rest32(y1, h1));
                 if (kFew) {
                     qa[i] = (g & 1) ? lo : hi;
                 } else {
