@@ -19,9 +19,9 @@
 //  * The probabilities go in as two f16 parts of 2^15 p, 22 bits of the fp32 value, absolute 2^-40 for small ones; a tile's products are added to the
 //    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates).  Up to four heads per group the eight columns hold the
 //    high and low parts of a head side by side, so that a lane has one head to exponentiate.
-//  * An arrival's answer is not waited for before the CTA's next part; the partials of a slab come to its last CTA through shared memory, 16 at a time.
-// What it takes (back to back, and what bounds it): one sequence of 2048 tokens 7.8 us, latency (wait 0.9, first rows 2.0, a tile 0.9, its warps
-// merged 0.6, arrival 0.9, merge 1.7); 80 slabs of 4.1K 19.4 us, 0.66 of the copy rate: head and tail of a launch, between them 7.5 TB/s into the SMs; 128 slabs of 8.2K
+//  * An arrival's answer is not waited for before the CTA's next part; the last CTA of a slab loads its partials 16 at a time.
+// What it takes (back to back, and what bounds it): one sequence of 2048 tokens 7.4 us, latency (wait 0.9, first rows 2.0, a tile 0.9, its warps
+// merged 0.6, arrival 0.9, merge 1.3); 80 slabs of 4.1K 19.4 us, 0.66 of the copy rate: head and tail of a launch, between them 7.5 TB/s into the SMs; 128 slabs of 8.2K
 // behind pages, int8, five heads 50.2 us, 0.81: conversions and latency; 128 slabs of 32K to 64K 240 us, 1.02, and 280 in seconds of it (power).
 #include <type_traits>
 
@@ -46,8 +46,7 @@ constexpr int kQdTableSlabs = 1024;                           // from so many sl
                                                               // with it and 31.7 without, 512 of 200 rows 15.9 and 15.3
 constexpr int kQdSumStride = kHeadDim + 4;                    // (of a column's sums in shared memory)
 static_assert(kQdStageBytes >= 8 * kQdSumStride * 4, "a warp's sums of a segment fit into a stage");
-constexpr int kQdMergeParts = kQdStageBytes / (kHeadDim * 4);   // partials of a head that are merged at a time
-static_assert(kQdMergeParts == 16, "half a warp");
+constexpr int kQdMergeParts = 16;                             // partials of a head that are merged at a time, half a warp
 static_assert((1ull << 22) * kQdMaxGrid <= (1ull << 32), "places times CTAs in 32 bits");
 static_assert(kQdThreads == kHeadDim, "a thread merges one channel");
 
@@ -693,10 +692,10 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
         }
         if (last) {
             // This CTA was the last to deliver a part of slab `done`: a warp takes a head, a lane a partial for the weights (maximum, sum) and four
-            // channels for the sums.  They come through shared memory (the warp's stage that is read out), so that all are on their way at once.
+            // channels for the sums; the loads of 16 partials are on their way at once (into registers; by way of shared memory: 7.9 us for one sequence of
+            // 2K against 7.4).
             const float* r0 = dec_part + size_t(done_cta + done) * n * kDecPartStride;
             const size_t stride = size_t(n) * kDecPartStride;
-            float* const to = sums(warp) + lane * 4;
 #pragma unroll 1
             for (int hl = warp; hl < n; hl += kQdWarps) {
                 const float* rh = r0 + hl * kDecPartStride;
@@ -707,9 +706,10 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                     const int cnt = min(kQdMergeParts, done_parts - p0);
                     const bool on = lane < cnt;
                     const float2 ml = __ldcg(reinterpret_cast<const float2*>(rh + size_t(p0 + min(lane, cnt - 1)) * stride + kHeadDim));
-#pragma unroll 4
-                    for (int k = 0; k < cnt; ++k) cp_async_piece(smem_u32(to + k * kHeadDim), rh + size_t(p0 + k) * stride + lane * 4);
-                    cp_async_commit();
+                    float4 part[kQdMergeParts];
+#pragma unroll
+                    for (int k = 0; k < kQdMergeParts; ++k)
+                        part[k] = k < cnt ? __ldcg(reinterpret_cast<const float4*>(rh + size_t(p0 + k) * stride) + lane) : make_float4(0.f, 0.f, 0.f, 0.f);
                     float mx = on ? ml.x : -INFINITY;
 #pragma unroll
                     for (int d = kQdMergeParts / 2; d; d >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, d));
@@ -722,13 +722,11 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                     L = fmaf(L, keep, __shfl_sync(0xffffffffu, ls, 0));
                     M = Mn;
                     A.x *= keep; A.y *= keep; A.z *= keep; A.w *= keep;
-                    cp_async_wait<0>();                   // (a lane reads what it copied)
-#pragma unroll 4
-                    for (int k = 0; k < cnt; ++k) {
+#pragma unroll
+                    for (int k = 0; k < kQdMergeParts; ++k) {
                         const float wk = __shfl_sync(0xffffffffu, w, k);
-                        const float4 a = *reinterpret_cast<const float4*>(to + k * kHeadDim);
-                        A.x = fmaf(a.x, wk, A.x); A.y = fmaf(a.y, wk, A.y);
-                        A.z = fmaf(a.z, wk, A.z); A.w = fmaf(a.w, wk, A.w);
+                        A.x = fmaf(part[k].x, wk, A.x); A.y = fmaf(part[k].y, wk, A.y);
+                        A.z = fmaf(part[k].z, wk, A.z); A.w = fmaf(part[k].w, wk, A.w);
                     }
                 }
                 const float inv = L == 0.f ? 0.f : 1.f / L;
