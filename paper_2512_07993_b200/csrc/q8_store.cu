@@ -95,8 +95,12 @@ __device__ __forceinline__ uint32_t without_nan(uint32_t w, uint32_t& fin) {
     }
     return h[0] | (h[1] << 16);
 }
-__device__ __forceinline__ float2 within(float2 v, float top) {      // an infinity: the largest code of its sign (e4m3 saturates by itself)
-    return make_float2(fminf(fmaxf(v.x, -top), top), fminf(fmaxf(v.y, -top), top));
+// int8: four values, infinities among them, times inv to codes: an infinity to the largest code of its sign (e4m3 saturates by itself).  It is held to
+// that behind the scaling, not before it: 127 times the largest scale, 2^122, is no number of 32 bits.
+__device__ __forceinline__ uint32_t codes4_wild(const uint2& x, float inv) {
+    auto held = [&](float v) { return fminf(fmaxf(v * inv, -127.f), 127.f); };
+    const float2 v0 = bf16x2_to_f2(x.x), v1 = bf16x2_to_f2(x.y);
+    return q8_round<SKIPKV_Q8_INT8>(held(v0.x), held(v0.y), held(v1.x), held(v1.y));
 }
 // Exponent of a scale that a block has: one that is no power of two goes to the next.
 __device__ __forceinline__ int held_exp(float s) {
@@ -274,10 +278,7 @@ q8_store_kernel(int n_slabs, StoreSlabs<kAppend> slabs, StoreArgs a, const int* 
             uint2* p = to + i * 2 * (kQ8RowBytes / 8);
             if (tok >= old) {
                 if (kFmt == SKIPKV_Q8_INT8 && wild) {
-                    const float top = 127.f * s_new;
-                    const float2 k2 = make_float2(inv, inv);
-                    *p = make_uint2(q8_round_scaled(within(bf16x2_to_f2(x[i].x), top), within(bf16x2_to_f2(x[i].y), top), k2),
-                                    q8_round_scaled(within(bf16x2_to_f2(x[i].z), top), within(bf16x2_to_f2(x[i].w), top), k2));
+                    *p = make_uint2(codes4_wild(make_uint2(x[i].x, x[i].y), inv), codes4_wild(make_uint2(x[i].z, x[i].w), inv));
                 } else {
                     *p = codes8<kFmt>(x[i], inv);
                 }
@@ -380,10 +381,9 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
             for (int i = 0; i < kQoRows; ++i) {
                 if (k0 + i >= take) break;
                 if (wild) { uint32_t fin = 0; y[i].x = without_nan(y[i].x, fin); y[i].y = without_nan(y[i].y, fin); }
-                float2 v0 = bf16x2_to_f2(y[i].x), v1 = bf16x2_to_f2(y[i].y);
-                if (kFmt == SKIPKV_Q8_INT8 && wild) { v0 = within(v0, 127.f * s_new); v1 = within(v1, 127.f * s_new); }
-                row[(k0 + i) * (kQ8RowBytes / 4)] = kFmt == SKIPKV_Q8_INT8 ? q8_round_scaled(v0, v1, make_float2(inv, inv))
-                                                                          : q8_round<kFmt>(v0.x * inv, v0.y * inv, v1.x * inv, v1.y * inv);
+                const float2 v0 = bf16x2_to_f2(y[i].x), v1 = bf16x2_to_f2(y[i].y);
+                row[(k0 + i) * (kQ8RowBytes / 4)] = kFmt != SKIPKV_Q8_INT8 ? q8_round<kFmt>(v0.x * inv, v0.y * inv, v1.x * inv, v1.y * inv)
+                                                    : wild ? codes4_wild(y[i], inv) : q8_round_scaled(v0, v1, make_float2(inv, inv));
             }
         }
         if (s_new == s_old) continue;
