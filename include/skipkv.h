@@ -440,7 +440,7 @@ int skipkv_decode_attn_static(const skipkv_shape* shape, const void* q, const vo
  * What the storing calls write: s is a power of two, the smallest that brings the largest finite magnitude of the block's rows to
  * at most 448 (E4M3) or 127 (INT8), 2^-100 at least; c = value / s rounded to nearest even.  An infinity is stored as the largest
  * code of its sign, a NaN as 0, and SKIPKV_STATUS_NOT_FINITE is raised.  Codes and scales are the same bits from run to run.
- * The reading calls take any positive scales, an append to a block those up to 2^122.  Rows that lie outside the buffers (a page that is
+ * The reading calls and an append to a block take any scales from 2^-111 to 2^122.  Rows that lie outside the buffers (a page that is
  * not in [0, rows / SKIPKV_PAGE_ROWS), a slab that reaches beyond `rows`) are neither read nor written: SKIPKV_STATUS_BAD_TABLE is
  * raised, and attention goes on without them.  Two slabs must not share a page that a call writes (reading a shared one is fine).  None of
  * these calls waits for anything on the GPU but the work before it on the stream: the wait limit does not concern them.  At most 8192
@@ -500,7 +500,8 @@ int skipkv_append_step_q8(const skipkv_shape* shape, const skipkv_q8_cache* cach
 
 /*
  * skipkv_decode_attn_q8 -- skipkv_decode_attn over an 8-bit cache: out[b][q] = sum_t softmax_t(q[b][q] . (s_k c_k)[t] / sqrt(d))
- * (s_v c_v)[t] for t < kv_len[b][q / n]; the codes take part as they are, sums and softmax are those of 32 bits; bf16 result;
+ * (s_v c_v)[t] for t < kv_len[b][q / n]; the codes take part as they are, sums and softmax are those of 32 bits (so logits and the sums of
+ * p_t |s_v c_v|, p_t relative to the largest probability, have to stay below 2^127); bf16 result;
  * kv_len == 0 gives zeros.  Lengths beyond a slab's room are taken as the room.  Everything else, the steering add included, as
  * skipkv_decode_attn.
  */

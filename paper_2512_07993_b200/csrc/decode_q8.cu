@@ -17,7 +17,7 @@
 //    which byte permutes make pairs of tokens.  Rows are 128 bytes; their 16-byte pieces lie permuted (piece c of row r at c ^ (r & 7)), so
 //    neither load has bank conflicts.
 //  * The probabilities go in as two f16 parts of 2^15 p, 22 bits of the fp32 value, absolute 2^-40 for small ones; a tile's products are added to the
-//    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates).  Up to four heads per group the eight columns hold the
+//    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates), times the scale and 2^-15: sums of p |v| may reach 2^127.  Up to four heads per group the eight columns hold the
 //    high and low parts of a head side by side, so that a lane has one head to exponentiate.
 //  * An arrival's answer is not waited for before the CTA's next part; the last CTA of a slab loads its partials 16 at a time.
 // What it takes (back to back, and what bounds it): one sequence of 2048 tokens 7.4 us, latency (wait 0.9, first rows 2.0, a tile 0.9, its warps
@@ -44,6 +44,7 @@ constexpr int kQdPartCost = 4;                                // what a slab cos
 constexpr int kQdPrefetch = 3;                                // tiles that a CTA starts towards L2 before it may read the cache
 constexpr int kQdTableSlabs = 1024;                           // from so many slabs on their table has a launch of its own: 1024 of 300 rows 29.8 us
                                                               // with it and 31.7 without, 512 of 200 rows 15.9 and 15.3
+constexpr float kQdUnit = 1.f / 32768.f;                      // what a probability of 2^15 stands for
 constexpr int kQdSumStride = kHeadDim + 4;                    // (of a column's sums in shared memory)
 static_assert(kQdStageBytes >= 8 * kQdSumStride * 4, "a warp's sums of a segment fit into a stage");
 constexpr int kQdMergeParts = 16;                             // partials of a head that are merged at a time, half a warp
@@ -599,7 +600,9 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                         for (int k = 0; k < 4; ++k)
                             if (16 * u + 2 * qd + (k & 1) + (k >> 1) * 8 >= rows_left) v[u][k] = make_uint4(0u, 0u, 0u, 0u);
                 }
-                const float2 vs2[2] = {make_float2(scales.z, scales.z), two ? make_float2(scales.w, scales.w) : make_float2(0.f, 0.f)};
+                // (the 2^15 of the probabilities comes off here, before the sums, whose range is that of 32 bits then)
+                const float vs0 = scales.z * kQdUnit, vs1 = two ? scales.w * kQdUnit : 0.f;
+                const float2 vs2[2] = {make_float2(vs0, vs0), make_float2(vs1, vs1)};
 #pragma unroll
                 for (int w = 0; w < 4; ++w) {
                     auto word = [&](int u, int k) { return w == 0 ? v[u][k].x : w == 1 ? v[u][k].y : w == 2 ? v[u][k].z : v[u][k].w; };
@@ -630,6 +633,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             l.x += __shfl_xor_sync(0xffffffffu, l.x, d);
             l.y += __shfl_xor_sync(0xffffffffu, l.y, d);
         }
+        l.x *= kQdUnit; l.y *= kQdUnit;
         // The heads' sums go to the stage of the tile that was worked on last: its rows are read out, and the next copy into it is issued behind
         // the barriers below.
         if (kFew) {

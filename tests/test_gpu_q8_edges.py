@@ -50,3 +50,46 @@ def test_infinities_beside_the_largest_magnitude(B, fmt, paged, block):
         assert b.item() == n
         same(c, 0, n, [codes] * 2, [scale] * 2)
         a, b = b, a
+
+
+# ------------------------------------------------------------------ attention near the ends of 32 bits
+def slab_cache(B, lens, hk, fmt, paged, k_scale, v_scale, seed, n_q, general=False):
+    """Slabs of ordinary codes whose scales are the given ones, times up to two."""
+    bt = len(lens)
+    c = Cache(B, lens, [int(max(x)) for x in lens], hk, fmt, 32, paged, seed, n_q=n_q)
+    codes, scales = ([], []), ([], [])
+    for s in range(bt * hk):
+        n = int(c.lens.reshape(-1)[s])
+        for i, base in enumerate((k_scale, v_scale)):
+            x, f = random_slab(c.r, n, 32, fmt)
+            f = np.full_like(f, base)
+            codes[i].append(x)
+            scales[i].append(np.asarray(f * c.r.uniform(1, 2, len(f)), np.float32).astype(np.float64) if general else f)
+    c.put(codes, scales)
+    c.rows64 = [[oracle.q8_rows(codes[i][s], scales[i][s], len(codes[i][s]), 32, fmt) for s in range(c.slabs)] for i in range(2)]
+    return c
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("group", [3, 7])
+def test_attention_over_values_near_the_largest(B, fmt, paged, group):
+    """Sums of p |v| (p relative to the largest) below 2^127, as a cache in 32 bits would have them: 600 rows of up to 448 * 2^108 < 2^117 (1e35), and
+    one row of the largest value there is."""
+    k = 2.0 ** -8 if fmt == "e4m3" else 2.0 ** -6
+    c = slab_cache(B, [[600, 77], [5000, 1]], 2, fmt, paged, k, 2.0 ** 108, 3, 2 * group)
+    q = queries(c, 2 * group, 7)
+    check_attention(c, q, attend(c, q))
+    c = slab_cache(B, [[1, 1]], 2, fmt, paged, k, 2.0 ** (118 if fmt == "e4m3" else 120), 3, 2 * group)
+    q = queries(c, 2 * group, 8)
+    check_attention(c, q, attend(c, q))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("general", [False, True])
+@pytest.mark.parametrize("group", [3, 7])
+def test_attention_over_the_least_scales(B, fmt, general, group):
+    """2^-111, where products with 2^-15 are normal numbers still, and queries that make ordinary logits of such keys."""
+    c = slab_cache(B, [[600, 77], [5000, 1]], 2, fmt, False, 2.0 ** -111, 2.0 ** -111, 3, 2 * group, general)
+    q = queries(c, 2 * group, 7, 2.0 ** (103 if fmt == "e4m3" else 105))
+    check_attention(c, q, attend(c, q))
