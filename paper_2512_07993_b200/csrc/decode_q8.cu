@@ -44,6 +44,7 @@ constexpr int kQdPartCost = 4;                                // what a slab cos
 constexpr int kQdPrefetch = 3;                                // tiles that a CTA starts towards L2 before it may read the cache
 constexpr int kQdTableSlabs = 1024;                           // from so many slabs on their table has a launch of its own: 1024 of 300 rows 29.8 us
                                                               // with it and 31.7 without, 512 of 200 rows 15.9 and 15.3
+constexpr float kQdLeast = -3.4028234663852886e38f;           // below no logit: the lowest finite number
 constexpr float kQdUnit = 1.f / 32768.f;                      // what a probability of 2^15 stands for
 constexpr int kQdSumStride = kHeadDim + 4;                    // (of a column's sums in shared memory)
 static_assert(kQdStageBytes >= 8 * kQdSumStride * 4, "a warp's sums of a segment fit into a stage");
@@ -669,7 +670,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
 #pragma unroll
             for (int hl = 0; hl < (kFew ? 4 : kMaxGroup); ++hl) {
                 if (hl >= n) break;
-                float M = -1e30f, L = 0.f, A = 0.f;       // (finite: a warp without rows has -inf)
+                float M = kQdLeast, L = 0.f, A = 0.f;     // (finite: a warp without rows has -inf)
 #pragma unroll
                 for (int w = 0; w < kQdWarps; ++w) M = fmaxf(M, s_ml[w][hl].x);
 #pragma unroll
@@ -704,7 +705,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             for (int hl = warp; hl < n; hl += kQdWarps) {
                 const float* rh = r0 + hl * kDecPartStride;
                 float4 A = make_float4(0.f, 0.f, 0.f, 0.f);
-                float M = -1e30f, L = 0.f;
+                float M = kQdLeast, L = 0.f;
 #pragma unroll 1
                 for (int p0 = 0; p0 < done_parts; p0 += kQdMergeParts) {
                     const int cnt = min(kQdMergeParts, done_parts - p0);

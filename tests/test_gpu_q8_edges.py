@@ -93,3 +93,23 @@ def test_attention_over_the_least_scales(B, fmt, general, group):
     c = slab_cache(B, [[600, 77], [5000, 1]], 2, fmt, False, 2.0 ** -111, 2.0 ** -111, 3, 2 * group, general)
     q = queries(c, 2 * group, 7, 2.0 ** (103 if fmt == "e4m3" else 105))
     check_attention(c, q, attend(c, q))
+
+
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("group", [2, 6])
+@pytest.mark.parametrize("n", [1, 100, 300, 9000])
+def test_attention_with_logits_far_below_zero(B, fmt, paged, group, n):
+    """Logits of -2^122 and below, all of them: the largest has all of the weight, wherever its row lies."""
+    c = slab_cache(B, [[n]], 1, fmt, paged, 1.0, 1.0, 5, group)
+    top = (n * 2) // 3
+    v = c.rows64[1][0]
+    codes = np.zeros((n, 128), np.uint8)
+    codes[:, 0] = oracle.q8_nearest(np.array([-64.0]), fmt)[0]
+    codes[top, 0] = oracle.q8_nearest(np.array([-32.0]), fmt)[0]
+    old = c.get(0, n)
+    c.put(([codes], [old[1][0]]), ([np.full(-(-n // 32), 2.0 ** 60)], [old[1][1]]))
+    q = torch.zeros(1, group, 128)
+    q[:, :, 0] = 2.0 ** 60
+    out = attend(c, q.bfloat16().cuda()).double().cpu().numpy()
+    assert np.array_equal(out[0], np.broadcast_to(bf16(v[top]).double().numpy(), (group, 128)))
