@@ -234,8 +234,9 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
     const int pages = int(c.rows / kQ8Tile);
     const size_t lane_off = size_t(warp * kQdRows + c_row) * kQ8RowBytes + c_col * 16;
     const int all_scales = c.table ? 0x7fffffff : n_slabs * c.max_blocks;
-    uint32_t skip = 0;                                    // stages without copies: no rows, or rows that lie outside the buffers
-    bool far = false;                                     // a copy was left out under the schedule from before the wait
+    uint32_t inside = 0;                                  // a byte for each stage: how many of its rows the buffers have (0: nothing was copied)
+    auto set_inside = [&](int rows) { inside = (inside & ~(0xffu << (8 * p_stage))) | (uint32_t(rows) << (8 * p_stage)); };
+    bool far = false;                                     // rows were left out under the schedule from before the wait
     auto copy_rows = [&](size_t off, const float* scale) {
         const uint8_t *kp = c.K + off, *vp = c.V + off;
         const uint32_t to = dst0 + p_stage * kQdStageBytes;
@@ -283,7 +284,7 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                 p_off += kQ8Tile * kQ8RowBytes;
                 p_sp += per_tile;
             }
-            skip &= ~(1u << p_stage);
+            set_inside(kQdRows);
             --p_fast;
             ++p_t;
             if (++p_stage == kQdStages) p_stage = 0;
@@ -296,9 +297,10 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
             const int place = c.table ? (uint32_t(p_page) < uint32_t(pages) ? p_page * per_tile + sub : 0) : p_slab * c.max_blocks + j * per_tile + sub;
             if (c.table && p_t + 1 < p_end) p_page = __ldcg(++p_table);
             const int rows = early ? kQdRows : min(p_rows, kQdRows);
-            const bool in = row + min(p_rows, kQdRows) <= int(c.rows);
-            skip &= ~(1u << p_stage);
-            if (rows > 0 && in && row < int(c.rows)) {
+            const int have = rows > 0 ? min(int(c.rows) - row, kQdRows) : 0;
+            const bool in = have >= min(p_rows, kQdRows);
+            set_inside(have);
+            if (have > 0) {
                 // all 32 rows, also where the slab has fewer left: what follows them is not used (zeros behind the buffer)
                 const size_t off = size_t(uint32_t(row + c_row)) * kQ8RowBytes + c_col * 16;
                 const float* scale = sp + min(place, all_scales - 1);
@@ -314,11 +316,9 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                     }
                     if (lane < 4) cp_async4(sp_dst + p_stage * 16, scale);
                 }
-            } else {
-                skip |= 1u << p_stage;
-                far = far || (early && !in);
-                if (lane == 0 && rows > 0 && !early) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
             }
+            far = far || (early && !in);
+            if (lane == 0 && !in && !early) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
             ++p_t;
             whole_tiles(j + 1);
             if (++p_stage == kQdStages) p_stage = 0;
@@ -465,12 +465,12 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
         for (; t < seg_end; ++t, rows_left -= kQ8Tile) {
             cp_async_wait<kQdStages - 2>();
             __syncwarp();                                 // every lane's pieces have landed; the stage before is read out
-            const bool live = rows_left > 0 && !((skip >> c_stage) & 1u);
+            const int rows = min(rows_left, int((inside >> (8 * c_stage)) & 0xffu));       // that this warp has of the tile
             issue_next(false);
-            if (live) {
+            if (rows > 0) {
                 const uint32_t so = c_stage * kQdStageBytes;
                 const float4 scales = *reinterpret_cast<const float4*>(s_scale[warp][c_stage]);
-                const bool two = rows_left > 16;          // the second group has rows
+                const bool two = rows > 16;               // the second group has rows
                 float s[2][2][4];                         // per group: two chains (int8), high and low parts (e4m3, many heads), one (few)
 #pragma unroll
                 for (int half = 0; half < 2; ++half)
@@ -518,12 +518,12 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                         for (int r = 0; r < 2; ++r)
                             x[u][r] = f * (kFmt == SKIPKV_Q8_E4M3 ? fmaf(s[u][0][2 * r + 1], 0.03125f, s[u][0][2 * r]) : s[u][0][2 * r] + s[u][1][2 * r]);
                     }
-                    if (rows_left < kQdRows) {            // the end of the slab: rows behind it hold anything, NaN too
+                    if (rows < kQdRows) {                 // the end of the slab: rows behind it hold anything, NaN too
 #pragma unroll
                         for (int u = 0; u < 2; ++u)
 #pragma unroll
                             for (int r = 0; r < 2; ++r)
-                                if (16 * u + 8 * r + g >= rows_left) x[u][r] = -INFINITY;
+                                if (16 * u + 8 * r + g >= rows) x[u][r] = -INFINITY;
                     }
                     float top = fmaxf(fmaxf(x[0][0], x[0][1]), fmaxf(x[1][0], x[1][1]));
                     if (__any_sync(0xffffffffu, top > m.x)) {
@@ -560,11 +560,11 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                         x[u] = __fmul2_rn(__ffma2_rn(a1, make_float2(part, part), a), f2);
                         y[u] = __fmul2_rn(__ffma2_rn(b1, make_float2(part, part), b), f2);
                     }
-                    if (rows_left < kQdRows) {
+                    if (rows < kQdRows) {
 #pragma unroll
                         for (int u = 0; u < 2; ++u) {
-                            if (16 * u + g >= rows_left) x[u] = make_float2(-INFINITY, -INFINITY);
-                            if (16 * u + 8 + g >= rows_left) y[u] = make_float2(-INFINITY, -INFINITY);
+                            if (16 * u + g >= rows) x[u] = make_float2(-INFINITY, -INFINITY);
+                            if (16 * u + 8 + g >= rows) y[u] = make_float2(-INFINITY, -INFINITY);
                         }
                     }
                     float2 top = make_float2(fmaxf(fmaxf(x[0].x, y[0].x), fmaxf(x[1].x, y[1].x)), fmaxf(fmaxf(x[0].y, y[0].y), fmaxf(x[1].y, y[1].y)));
@@ -594,12 +594,12 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
                     }
                     l = __fadd2_rn(l, __fadd2_rn(__fadd2_rn(x[0], y[0]), __fadd2_rn(x[1], y[1])));
                 }
-                if (rows_left < kQdRows) {
+                if (rows < kQdRows) {
 #pragma unroll
                     for (int u = 0; u < 2; ++u)
 #pragma unroll
                         for (int k = 0; k < 4; ++k)
-                            if (16 * u + 2 * qd + (k & 1) + (k >> 1) * 8 >= rows_left) v[u][k] = make_uint4(0u, 0u, 0u, 0u);
+                            if (16 * u + 2 * qd + (k & 1) + (k >> 1) * 8 >= rows) v[u][k] = make_uint4(0u, 0u, 0u, 0u);
                 }
                 // (the 2^15 of the probabilities comes off here, before the sums, whose range is that of 32 bits then)
                 const float vs0 = scales.z * kQdUnit, vs1 = two ? scales.w * kQdUnit : 0.f;

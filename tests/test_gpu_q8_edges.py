@@ -113,3 +113,20 @@ def test_attention_with_logits_far_below_zero(B, fmt, paged, group, n):
     q[:, :, 0] = 2.0 ** 60
     out = attend(c, q.bfloat16().cuda()).double().cpu().numpy()
     assert np.array_equal(out[0], np.broadcast_to(bf16(v[top]).double().numpy(), (group, 128)))
+
+
+# ------------------------------------------------------------------ slabs that reach beyond the buffers
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("inside", [0, 1, 17, 31, 32, 33, 100, 127, 128, 129, 160, 299, -20])
+def test_attention_over_the_rows_inside_the_buffer(B, fmt, inside):
+    """A slab of which the buffer has the first rows only: those are attended to, however few of a tile they are, and it is reported."""
+    c = filled(B, [[200, 250], [300, 301]], [256, 301], 2, fmt, 16, False, 5, n_q=6)
+    rows = c.row0[3] + inside
+    c.cache = B.make_q8_cache(c.K[:rows].view(DT[fmt]), c.V[:rows].view(DT[fmt]), c.ks, c.vs, 16)
+    for i in range(2):
+        c.rows64[i][3] = c.rows64[i][3][:max(inside, 0)]
+        c.rows64[i][2] = c.rows64[i][2][:min(300, rows - c.row0[2])]
+    q = queries(c, 6, 1)
+    check_attention(c, q, attend(c, q))
+    assert c.status() == 4
+    check_attention(c, q, attend(c, q))
