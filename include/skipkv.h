@@ -433,7 +433,8 @@ int skipkv_decode_attn_static(const skipkv_shape* shape, const void* q, const vo
  *
  * Two layouts, as in 16 bits:
  *   contiguous slabs (block_table NULL): row of (b, h, t) as above, 128 bytes per row; the scale of block i of slab (b, h) at
- *     k_scale[(b * Hk + h) * max_blocks + i].  A slab has room for min(cap[b], max_blocks * block_rows) tokens.
+ *     k_scale[(b * Hk + h) * max_blocks + i].  A slab has room for min(cap[b], max_blocks * block_rows) tokens, and for no more than
+ *     lie in front of the buffers' end.
  *   paged (block_table device int32 [batch][Hk][max_pages]): token t in row t % SKIPKV_PAGE_ROWS of page
  *     block_table[b][h][t / SKIPKV_PAGE_ROWS], 16 KB per page and tensor; the scales lie by page, block i of page p at
  *     k_scale[p * (SKIPKV_PAGE_ROWS / block_rows) + i].  A slab has room for min(cap[b], max_pages * SKIPKV_PAGE_ROWS) tokens.
@@ -442,7 +443,7 @@ int skipkv_decode_attn_static(const skipkv_shape* shape, const void* q, const vo
  * code of its sign, a NaN as 0, and SKIPKV_STATUS_NOT_FINITE is raised.  Codes and scales are the same bits from run to run.
  * The reading calls and an append to a block take any scales from 2^-111 to 2^122.  Rows that lie outside the buffers (a page that is
  * not in [0, rows / SKIPKV_PAGE_ROWS), a slab that reaches beyond `rows`) are neither read nor written: SKIPKV_STATUS_BAD_TABLE is
- * raised, and attention goes on without them.  Two slabs must not share a page that a call writes (reading a shared one is fine).  None of
+ * raised, and attention and skipkv_unpack_q8 go on with the others.  Two slabs must not share a page that a call writes (reading a shared one is fine).  None of
  * these calls waits for anything on the GPU but the work before it on the stream: the wait limit does not concern them.  At most 8192
  * slabs, and fewer than 2^30 scales in a table of contiguous slabs or entries in a block table (SKIPKV_ERR_UNSUPPORTED).
  */
@@ -468,7 +469,7 @@ typedef struct {
 /*
  * skipkv_pack_q8 -- the live rows of bf16 slabs into an 8-bit cache, from each slab's first block on: what a program does with
  * a layer when its eviction pass is done.  K, V: device bf16, contiguous slabs of `shape` (read only; shape->total_rows is their row
- * count).  kv_len: device [batch][Hk].  A slab with more rows than the cache has room for is left out, and
+ * count).  kv_len: device [batch][Hk].  A slab with more rows than the cache has room for, or K and V hold, is left out, and
  * SKIPKV_STATUS_BAD_TABLE is raised.  Rows and scales behind the live ones are not written.
  */
 int skipkv_pack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* K, const void* V,
@@ -513,7 +514,7 @@ int skipkv_decode_attn_q8(const skipkv_shape* shape, const skipkv_q8_cache* cach
  * skipkv_unpack_q8 -- the live rows of an 8-bit cache as bf16 slabs, for the calls that read 16 bits: scoring and compaction
  * of a layer (then skipkv_pack_q8 again).  K[row of (b, h, t)] = bf16(s_k c_k), rounded to nearest even, for t < kv_len[b][h]; V the
  * same.  K, V: device bf16, contiguous slabs of `shape`, shape->total_rows rows; either may be NULL.  Other rows are not written.
- * A length beyond the slab's room is taken as the room, one below zero as zero, and SKIPKV_STATUS_BAD_TABLE is raised.
+ * A length beyond the slab's room, there or in K and V, is taken as the room, one below zero as zero, and SKIPKV_STATUS_BAD_TABLE is raised.
  */
 int skipkv_unpack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const int32_t* kv_len, void* K, void* V,
                      void* ws, void* stream);

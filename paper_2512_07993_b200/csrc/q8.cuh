@@ -46,6 +46,15 @@ __host__ __device__ __forceinline__ int q8_row0(int64_t off, int cap, int Hk, in
 __host__ __device__ __forceinline__ int q8_row0(const int64_t* slab_off, const int32_t* cap, int Hk, int s) {
     return q8_row0(slab_off[s / Hk], cap[s / Hk], Hk, s);
 }
+// What of `room` rows from row0 on (as q8_row0 gives it) a buffer of `rows` rows has.
+__host__ __device__ __forceinline__ int rows_inside(int room, int row0, long long rows) {
+    return row0 < 0 ? 0 : int(max(0ll, min((long long)room, rows - row0)));
+}
+// Rows that slab s has room for, in the buffers too where it is contiguous.
+__host__ __device__ __forceinline__ int q8_room_inside(const Q8View& v, int cap, int row0) {
+    const int room = q8_room(v, cap);
+    return v.table ? room : rows_inside(room, row0, v.rows);
+}
 // Where tile j (tokens [128 j, 128 j + 128)) of slab s lies: its first row, and the place of its first block's scale.  Of its first
 // `rows` rows none may lie outside the buffers, else row = -1.  row0: as q8_row0 gives it (not used for a paged cache).
 struct Q8Tile { long long row; size_t scale; };

@@ -124,9 +124,9 @@ struct StoreSlabs {
         return {kAppend ? new_off[b] : 0, kAppend ? new_off[b + 1] : 0, len_in[s], cap[b], slab_off[b]};
     }
     __device__ __forceinline__ Span span(int s, const Raw& r) const {
-        const int room = q8_room(c, r.cap);
         Span x;
         x.row0 = q8_row0(r.off, r.cap, Hk, s);
+        const int room = q8_room_inside(c, r.cap, x.row0);
         if (kAppend) {
             x.old = r.len;
             x.bad = r.len < 0 || r.lo < 0 || r.hi < r.lo || r.hi > n_new || (long long)r.len + (r.hi - r.lo) > room;
@@ -330,7 +330,7 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
     const int s = w / (2 * kParts), part = (w >> 1) & (kParts - 1), b = s / Hk, block = 1 << c.block_log2;
     const int lo = a.new_off ? a.new_off[b] : b, hi = a.new_off ? a.new_off[b + 1] : b + 1;
     const int row0 = c.table ? 0 : q8_row0(slab_off, cap, Hk, s);        // (read beside the length)
-    const int old = a.len_in[s], room = q8_room(c, cap, Hk, s);
+    const int old = a.len_in[s], room = q8_room_inside(c, cap[b], row0);
     const bool fits = old >= 0 && lo >= 0 && hi >= lo && hi <= a.n_new && (long long)old + (hi - lo) <= room;
     const int count = fits ? hi - lo : 0;
     if (!fits && lane == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
@@ -463,10 +463,11 @@ struct LoadSlabs {
     const int32_t *cap, *kv_len;
     uint32_t* status;
     int Hk;
+    long long dst_rows;                                       // of the bf16 buffers
     __device__ __forceinline__ Raw load(int s) const { return {kv_len[s], cap[s / Hk], slab_off[s / Hk]}; }
     __device__ __forceinline__ Span span(int s, const Raw& r) const {
-        const int room = min(q8_room(c, r.cap), r.cap);
-        return {0, min(max(r.len, 0), max(room, 0)), q8_row0(r.off, r.cap, Hk, s), r.len < 0 || r.len > room};
+        const int row0 = q8_row0(r.off, r.cap, Hk, s), room = rows_inside(q8_room_inside(c, r.cap, row0), row0, dst_rows);
+        return {0, min(max(r.len, 0), room), row0, r.len < 0 || r.len > room};
     }
     __device__ __forceinline__ int count(int s, const Raw& r) const {
         const Span x = span(s, r);
@@ -477,7 +478,7 @@ struct LoadSlabs {
 
 template <int kFmt, bool kTable>
 __global__ void __launch_bounds__(kQsThreads, 6)
-q8_load_kernel(int n_slabs, LoadSlabs slabs, uint4* K, uint4* V, long long dst_rows, const int* slab_table) {
+q8_load_kernel(int n_slabs, LoadSlabs slabs, uint4* K, uint4* V, const int* slab_table) {
     extern __shared__ __align__(16) uint8_t qsm[];
     int* pref = reinterpret_cast<int*>(qsm);
     int* lens = pref + n_slabs + 1;                           // (not kTable)
@@ -515,7 +516,7 @@ q8_load_kernel(int n_slabs, LoadSlabs slabs, uint4* K, uint4* V, long long dst_r
         const int j = t - pref[s], rows = min(x_s.now - j * kQ8Tile, kQ8Tile);
         const Q8Tile at = q8_tile(c, s, j, rows, x_s.row0);
         const long long to = (long long)x_s.row0 + (long long)j * kQ8Tile;
-        if (at.row < 0 || x_s.row0 < 0 || to + rows > dst_rows) {
+        if (at.row < 0) {
             if (tid == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
             continue;
         }
@@ -676,12 +677,12 @@ extern "C" int skipkv_unpack_q8(const skipkv_shape* shape, const skipkv_q8_cache
     const bool table = n_slabs >= kQsTableSlabs;
     int* slab_table = reinterpret_cast<int*>(static_cast<uint8_t*>(ws) + make_layout(*shape).slab_table);
     cudaStream_t st = static_cast<cudaStream_t>(stream);
-    const LoadSlabs slabs{q8_view(*cache), shape->slab_off, shape->cap, kv_len, &static_cast<Header*>(ws)->status, int(shape->n_kv_heads)};
+    const LoadSlabs slabs{q8_view(*cache), shape->slab_off, shape->cap, kv_len, &static_cast<Header*>(ws)->status, int(shape->n_kv_heads),
+                          static_cast<long long>(shape->total_rows)};
     if (table) SKIPKV_CUDA(launch_dependent(q8_table_kernel<LoadSlabs>, dim3(1), dim3(kQ8TableThreads), 0, st, n_slabs, slabs, slab_table));
     auto run = [&](auto kernel) {
         return launch_dependent(kernel, dim3(store_grid(tiles, 6)), dim3(kQsThreads), size_t(table ? n_slabs + 1 : 3 * n_slabs + 1) * 4, st, n_slabs,
-                                slabs, static_cast<uint4*>(K), static_cast<uint4*>(V), static_cast<long long>(shape->total_rows),
-                                static_cast<const int*>(slab_table));
+                                slabs, static_cast<uint4*>(K), static_cast<uint4*>(V), static_cast<const int*>(slab_table));
     };
     auto pick = [&](auto fmt) {
         constexpr int kFmt = decltype(fmt)::value;

@@ -130,3 +130,76 @@ def test_attention_over_the_rows_inside_the_buffer(B, fmt, inside):
     check_attention(c, q, attend(c, q))
     assert c.status() == 4
     check_attention(c, q, attend(c, q))
+
+
+@pytest.mark.parametrize("many", [False, True])
+@pytest.mark.parametrize("inside", [0, 1, 100, 128, 149, -20, -60])
+def test_slabs_have_no_room_beyond_the_buffer(B, many, inside):
+    """Slabs that would reach beyond the buffer: packing leaves them out, appending leaves them and their lengths as they were, loading takes the rows
+    that are there; all report it."""
+    bt, fmt = 2100 if many else 2, "int8"
+    lens, caps = np.zeros(bt, np.int64), np.ones(bt, np.int64)
+    lens[-2:], caps[-2:] = 150, 200
+    c = filled(B, lens[:, None], caps, 1, fmt, 32, False, 5)
+    rows = c.row0[-1] + inside
+    room = np.minimum(caps, np.maximum(rows - np.array(c.row0), 0))
+    state = (c.K, c.V, c.ks.view(torch.int32), c.vs.view(torch.int32))
+    before = [x.clone() for x in state]
+    c.cache = B.make_q8_cache(c.K[:rows].view(DT[fmt]), c.V[:rows].view(DT[fmt]), c.ks, c.vs, 32)
+
+    def changed_alone(first, last):
+        """Rows [first, last) of the slabs and the scales of those that have any are other ones; the rest is what it was.  Then all is put back."""
+        for x, y in zip(state[:2], before):
+            keep = torch.ones(len(x), dtype=torch.bool, device="cuda")
+            for s in np.flatnonzero(last > first):
+                at = slice(c.row0[s] + int(first[s]), c.row0[s] + int(last[s]))
+                assert bool((x[at] != y[at]).any(1).all())
+                keep[at] = False
+            assert torch.equal(x[keep], y[keep])
+        same_scales = torch.from_numpy(last <= first).cuda()
+        for x, y in zip(state[2:], before[2:]):
+            assert torch.equal(x[same_scales], y[same_scales])
+        for x, y in zip(state, before):
+            x.copy_(y)
+
+    src = torch.full((c.rows16, 128), 2.0 ** -40, dtype=torch.bfloat16, device="cuda")
+    B.skipkv_pack_q8(c.shape, c.cache, src, src, c.kv_len, c.ws)
+    torch.cuda.synchronize()
+    assert c.status() == 4
+    changed_alone(np.zeros(bt, int), np.where(lens <= room, lens, 0))
+    # a few rows, without tiles, and so many (most of no sequence) that they go by tiles
+    for extra in (0, 4 * bt):
+        count = np.where(lens > 0, 2, 0)
+        off = torch.from_numpy(np.concatenate([[0], np.cumsum(count)]).astype(np.int32)).cuda()
+        n = int(count.sum()) + extra
+        x = torch.full((n, 1, 128), 2.0 ** -40, dtype=torch.bfloat16, device="cuda")
+        out = torch.full_like(c.kv_len, -1)
+        B.skipkv_append_q8(c.shape, c.cache, x, x, off, n, c.kv_len, out, c.ws)
+        torch.cuda.synchronize()
+        assert c.status() == 4
+        want = np.where(lens + count <= room, lens + count, lens)
+        assert np.array_equal(out.view(-1).cpu().numpy(), want)
+        changed_alone(lens, want)
+
+    def loaded(i):
+        y = np.full((c.rows16, 128), 7.0)
+        for s in np.flatnonzero(lens):
+            m = min(int(lens[s]), int(room[s]))
+            y[c.row0[s]:c.row0[s] + m] = c.rows64[i][s][:m]
+        return y
+
+    # the codes' buffer ends, then the one that they are loaded into
+    whole = B.make_q8_cache(c.K.view(DT[fmt]), c.V.view(DT[fmt]), c.ks, c.vs, 32)
+    short = B.make_shape(bt, 1, 1, 128, 1, 0, 1, c.max_cap, c.slab_off, c.cap, rows)
+    for shape, cache in ((c.shape, c.cache), (short, whole)):
+        back = [torch.full((c.rows16, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        B.skipkv_unpack_q8(shape, cache, c.kv_len, back[0], back[1], c.ws)
+        torch.cuda.synchronize()
+        assert c.status() == 4
+        for i in range(2):
+            assert np.array_equal(back[i].double().cpu().numpy(), loaded(i))
+    # bf16 slabs that reach beyond their buffer are not packed
+    B.skipkv_pack_q8(short, whole, src, src, c.kv_len, c.ws)
+    torch.cuda.synchronize()
+    assert c.status() == 4
+    changed_alone(np.zeros(bt, int), np.where(lens <= room, lens, 0))
