@@ -492,7 +492,8 @@ int skipkv_append_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, co
 /*
  * skipkv_append_step_q8 -- skipkv_append_step into an 8-bit cache: one token of each sequence is appended as by skipkv_append_q8
  * (new_off NULL), and the range list and the observation window are updated as by skipkv_append_step.  Lengths go from kv_len_in
- * to kv_len_out, a different buffer.
+ * to kv_len_out, a different buffer.  A slab whose n_sent is outside [0, max_sent] is left as it is, its length too, and
+ * SKIPKV_STATUS_BAD_TABLE is raised.
  */
 int skipkv_append_step_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, const void* k_new, const void* v_new,
                           const int32_t* kv_len_in, int32_t* kv_len_out, int32_t* sent_off, int32_t* sent_id,

@@ -331,7 +331,9 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
     const int lo = a.new_off ? a.new_off[b] : b, hi = a.new_off ? a.new_off[b + 1] : b + 1;
     const int row0 = c.table ? 0 : q8_row0(slab_off, cap, Hk, s);        // (read beside the length)
     const int old = a.len_in[s], room = q8_room_inside(c, cap[b], row0);
-    const bool fits = old >= 0 && lo >= 0 && hi >= lo && hi <= a.n_new && (long long)old + (hi - lo) <= room;
+    // (read beside the length too.  The slab's other warp may have added the sentence that this token opens: the count is a good one all the same)
+    const int S0 = a.n_sent != nullptr ? a.n_sent[s] : 0;
+    const bool fits = old >= 0 && lo >= 0 && hi >= lo && hi <= a.n_new && (long long)old + (hi - lo) <= room && S0 >= 0 && S0 <= a.max_sent;
     const int count = fits ? hi - lo : 0;
     if (!fits && lane == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
     const uint2* const src = reinterpret_cast<const uint2*>((w & 1) ? a.v_src : a.k_src) + (size_t(fits ? lo : 0) * Hk + s % Hk) * 32 + lane;
@@ -409,14 +411,12 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
     // ---- the length, and the rest of a decode step
     const int now = old + count;
     if (lane == 0) a.len_out[s] = now;
-    if (a.n_sent == nullptr) return;
-    const int S0 = a.n_sent[s];
-    const bool ok = S0 >= 0 && S0 <= a.max_sent, opens = S0 == 0 || a.new_sent[b];
+    if (a.n_sent == nullptr || !fits) return;                 // (no room, or a list that makes no sense: reported above, tables as they were)
+    const bool opens = S0 == 0 || a.new_sent[b];
     int32_t* so = a.sent_off + size_t(s) * (a.max_sent + 1);
-    const int S = ok && opens && S0 < a.max_sent ? S0 + 1 : S0;         // (a full list: the token joins the last sentence)
+    const int S = opens && S0 < a.max_sent ? S0 + 1 : S0;     // (a full list: the token joins the last sentence)
     __syncwarp();
-    if (lane == 0 && (!ok || (fits && opens && S == S0))) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
-    if (!ok || !fits) return;                                 // (no room: reported above, tables as they were)
+    if (lane == 0 && opens && S == S0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
     if (lane == 0 && S != S0) {
         if (S0 == 0) so[0] = 0;
         a.sent_id[size_t(s) * a.max_sent + S0] = a.gen_id[b];

@@ -203,3 +203,42 @@ def test_slabs_have_no_room_beyond_the_buffer(B, many, inside):
     torch.cuda.synchronize()
     assert c.status() == 4
     changed_alone(np.zeros(bt, int), np.where(lens <= room, lens, 0))
+
+
+# ------------------------------------------------------------------ range lists that make no sense
+@pytest.mark.parametrize("fmt", FORMATS)
+@pytest.mark.parametrize("paged", [False, True])
+def test_append_step_with_a_bad_sentence_count(B, fmt, paged):
+    """As skipkv_append_step beside a bf16 cache: reported, the length and the list as they were, the other slabs served.  The block's codes and scale
+    stay too, although the row would raise it."""
+    bt, hk, ms = 3, 2, 4
+    c = filled(B, [[5, 20], [7, 8], [16, 9]], [40] * bt, hk, fmt, 16, paged, 3, window=2, max_sent=ms)
+    row0 = [s * 40 for s in range(bt * hk)]
+    ref = B.make_shape(bt, hk, hk, 128, 2, 0, ms, 40, torch.tensor([0, 40, 80]).cuda(), torch.tensor([40] * bt, dtype=torch.int32).cuda(), 40 * bt * hk)
+    K16 = torch.zeros(40 * bt * hk, 128, dtype=torch.bfloat16, device="cuda")
+    counts = torch.tensor([[-1, 1], [ms + 1, 2], [ms, 1 << 30]], dtype=torch.int32)
+    mk = lambda: (torch.full((bt, hk, ms + 1), 77, dtype=torch.int32, device="cuda"), torch.full((bt, hk, ms), -1, dtype=torch.int32, device="cuda"),  # noqa: E731
+                  counts.clone().cuda())
+    a, b = mk(), mk()
+    len16, out = c.kv_len.clone(), torch.full_like(c.kv_len, -1)
+    x = torch.full((bt, hk, 128), 1000.0, dtype=torch.bfloat16, device="cuda")
+    opens, gid = torch.tensor([1, 0, 0], dtype=torch.uint8).cuda(), torch.full((bt,), 5, dtype=torch.int32, device="cuda")
+    before = [c.get(s, int(c.lens.reshape(-1)[s])) for s in range(c.slabs)]
+    B.skipkv_append_step(ref, K16, K16.clone(), x, x, len16, a[0], a[1], a[2], opens, gid, None, None, 0, c.ws)
+    torch.cuda.synchronize()
+    assert c.status() == 4
+    B.skipkv_append_step_q8(c.shape, c.cache, x, x, c.kv_len, out, b[0], b[1], b[2], opens, gid, None, None, 0, c.ws)
+    torch.cuda.synchronize()
+    assert c.status() == 4
+    for u, v in zip(a, b):
+        assert torch.equal(u, v)
+    assert torch.equal(out, len16)
+    ok = (counts >= 0) & (counts <= ms)
+    assert torch.equal(out.cpu(), torch.from_numpy(c.lens) + ok.int())
+    for s in range(c.slabs):
+        n = int(c.lens.reshape(-1)[s])
+        if ok.view(-1)[s]:
+            assert all((row[0][n] == row[0][n][0]).all() for row in c.get(s, n + 1))
+        else:
+            for (x0, f0), (x1, f1) in zip(before[s], c.get(s, n)):
+                assert np.array_equal(x0, x1) and np.array_equal(f0, f1)
