@@ -316,7 +316,8 @@ constexpr int kQoParts = 4;                                    // with more rows
 constexpr int kQoRows = 8;                                     // rows of new tokens on their way at a time
 constexpr int kQoHeld = 16;                                    // and of rows that a block had
 
-template <int kFmt, int kParts>
+// kStep: a decode step, one row to each sequence.
+template <int kFmt, int kParts, bool kStep>
 __global__ void __launch_bounds__(kQoThreads)
 q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, const int32_t* cap, Q8View c, StoreArgs a, uint32_t* status) {
     const int lane = threadIdx.x & 31, w = (blockIdx.x * kQoThreads + threadIdx.x) >> 5;
@@ -324,16 +325,18 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
     pdl_wait();
     if (w >= 2 * kParts * n_slabs) {                          // the step's queries into their slot of the window
         const int i = (w - 2 * kParts * n_slabs) * 32 + lane;
-        if (a.q_win != nullptr && i < batch * a.Hq * 16) a.q_win[(size_t(i >> 4) * a.window + a.slot) * 16 + (i & 15)] = a.q[i];
+        if (kStep && a.q_win != nullptr && i < batch * a.Hq * 16) a.q_win[(size_t(i >> 4) * a.window + a.slot) * 16 + (i & 15)] = a.q[i];
         return;
     }
     const int s = w / (2 * kParts), part = (w >> 1) & (kParts - 1), b = s / Hk, block = 1 << c.block_log2;
     const int lo = a.new_off ? a.new_off[b] : b, hi = a.new_off ? a.new_off[b + 1] : b + 1;
     const int row0 = c.table ? 0 : q8_row0(slab_off, cap, Hk, s);        // (read beside the length)
-    const int old = a.len_in[s], room = q8_room_inside(c, cap[b], row0);
+    const int old = a.len_in[s], room = q8_room(c, cap, Hk, s);
     // (read beside the length too.  The slab's other warp may have added the sentence that this token opens: the count is a good one all the same)
-    const int S0 = a.n_sent != nullptr ? a.n_sent[s] : 0;
-    const bool fits = old >= 0 && lo >= 0 && hi >= lo && hi <= a.n_new && (long long)old + (hi - lo) <= room && S0 >= 0 && S0 <= a.max_sent;
+    const int S0 = kStep ? a.n_sent[s] : 0;
+    const long long end = (long long)old + (hi - lo);
+    const bool inside = c.table != nullptr || (row0 >= 0 && end <= c.rows - row0);       // (with the room as q8_room_inside: a shorter chain)
+    const bool fits = old >= 0 && lo >= 0 && hi >= lo && hi <= a.n_new && end <= room && inside && (!kStep || (S0 >= 0 && S0 <= a.max_sent));
     const int count = fits ? hi - lo : 0;
     if (!fits && lane == 0) atomicOr(status, SKIPKV_STATUS_BAD_TABLE);
     const uint2* const src = reinterpret_cast<const uint2*>((w & 1) ? a.v_src : a.k_src) + (size_t(fits ? lo : 0) * Hk + s % Hk) * 32 + lane;
@@ -411,7 +414,7 @@ q8_append_few_kernel(int batch, int Hk, int n_slabs, const int64_t* slab_off, co
     // ---- the length, and the rest of a decode step
     const int now = old + count;
     if (lane == 0) a.len_out[s] = now;
-    if (a.n_sent == nullptr || !fits) return;                 // (no room, or a list that makes no sense: reported above, tables as they were)
+    if (!kStep || !fits) return;                              // (no room, or a list that makes no sense: reported above, tables as they were)
     const bool opens = S0 == 0 || a.new_sent[b];
     int32_t* so = a.sent_off + size_t(s) * (a.max_sent + 1);
     const int S = opens && S0 < a.max_sent ? S0 + 1 : S0;     // (a full list: the token joins the last sentence)
@@ -620,7 +623,8 @@ static int append(const skipkv_shape* shape, const skipkv_q8_cache* cache, const
     };
     auto pick = [&](auto fmt) {
         constexpr int kFmt = decltype(fmt)::value;
-        return parts ? run(q8_append_few_kernel<kFmt, kQoParts>) : run(q8_append_few_kernel<kFmt, 1>);
+        if (a.n_sent) return run(q8_append_few_kernel<kFmt, 1, true>);
+        return parts ? run(q8_append_few_kernel<kFmt, kQoParts, false>) : run(q8_append_few_kernel<kFmt, 1, false>);
     };
     SKIPKV_CUDA(cache->format == SKIPKV_Q8_E4M3 ? pick(std::integral_constant<int, SKIPKV_Q8_E4M3>()) : pick(std::integral_constant<int, SKIPKV_Q8_INT8>()));
     return SKIPKV_OK;
