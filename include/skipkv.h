@@ -464,6 +464,9 @@ typedef struct {
     float*  k_scale;      /* device                                                             */
     float*  v_scale;
     const int32_t* block_table;   /* device, or NULL: contiguous slabs                          */
+    int32_t batch;        /* sequences that the scales (contiguous) or the block table are laid out for; a call
+                             with more of them, or with other KV heads, is refused; both 0: not checked */
+    int32_t n_kv_heads;   /* KV heads of the same                                               */
 } skipkv_q8_cache;
 
 /*

@@ -57,7 +57,8 @@ class Params(C.Structure):
 class Q8Cache(C.Structure):
     _fields_ = [("format", C.c_int32), ("block_rows", C.c_int32), ("max_blocks", C.c_int32), ("max_pages", C.c_int32),
                 ("device", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("K", C.c_void_p), ("V", C.c_void_p),
-                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("block_table", C.c_void_p)]
+                ("k_scale", C.c_void_p), ("v_scale", C.c_void_p), ("block_table", C.c_void_p), ("batch", C.c_int32),
+                ("n_kv_heads", C.c_int32)]
 
 
 def lib():
@@ -136,7 +137,8 @@ def make_q8_cache(K: torch.Tensor, V: torch.Tensor, k_scale: torch.Tensor, v_sca
     """One layer's cache in 8 bits, as the ``_q8`` calls take it (it keeps the tensors alive).
 
     K, V: codes [rows][128], ``torch.float8_e4m3fn`` or ``torch.int8`` (which says how they are read).  Scales: float32,
-    [batch][Hk][max_blocks] for contiguous slabs, [pages][128 / block_rows] with a block table (int32 [batch][Hk][max_pages])."""
+    [batch][Hk][max_blocks] for contiguous slabs, [pages][128 / block_rows] with a block table (int32 [batch][Hk][max_pages]).  A call with
+    more sequences than that, or with other KV heads, is refused."""
     if K.dtype not in Q8_FORMATS or V.dtype != K.dtype:
         raise ValueError(f"codes are torch.float8_e4m3fn or torch.int8, K and V alike: got {K.dtype}, {V.dtype}")
     if K.dim() != 2 or K.shape[1] != 128 or K.shape != V.shape:
@@ -158,8 +160,9 @@ def make_q8_cache(K: torch.Tensor, V: torch.Tensor, k_scale: torch.Tensor, v_sca
     tensors = (K, V, k_scale, v_scale) + (() if block_table is None else (block_table,))
     if len({t.device for t in tensors}) != 1:
         raise ValueError("the tensors of one cache are on one device")
+    batch, heads = (k_scale if block_table is None else block_table).shape[:2]
     c = Q8Cache(Q8_FORMATS[K.dtype], block_rows, max_blocks, max_pages, K.device.index if K.is_cuda else -1, 0, K.shape[0], _ptr(K), _ptr(V),
-                _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), _ptr(block_table, torch.int32))
+                _ptr(k_scale, torch.float32), _ptr(v_scale, torch.float32), _ptr(block_table, torch.int32), batch, heads)
     c._keepalive = tensors
     return c
 

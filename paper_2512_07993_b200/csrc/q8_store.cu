@@ -548,6 +548,10 @@ int check_q8(const skipkv_shape* s, const skipkv_q8_cache* c) {
     if (c->block_rows != 16 && c->block_rows != 32 && c->block_rows != 64 && c->block_rows != 128) return SKIPKV_ERR_UNSUPPORTED;
     if ((reinterpret_cast<uintptr_t>(c->K) | reinterpret_cast<uintptr_t>(c->V)) & 15) return SKIPKV_ERR_INVALID_ARG;
     if ((reinterpret_cast<uintptr_t>(c->k_scale) | reinterpret_cast<uintptr_t>(c->v_scale)) & 3) return SKIPKV_ERR_INVALID_ARG;
+    if ((c->batch || c->n_kv_heads) && (c->batch < s->batch || c->n_kv_heads != s->n_kv_heads)) {
+        set_error_text("the 8-bit cache is laid out for fewer sequences, or for other KV heads");
+        return SKIPKV_ERR_INVALID_ARG;
+    }
     if (c->block_table ? c->max_pages <= 0 || c->rows % kQ8Tile != 0 : c->max_blocks <= 0) return SKIPKV_ERR_INVALID_ARG;
     if (c->rows > int64_t(0x7fffffff) - 256) return SKIPKV_ERR_UNSUPPORTED;
     const int64_t slabs = int64_t(s->batch) * s->n_kv_heads;

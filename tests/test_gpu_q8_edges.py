@@ -242,3 +242,22 @@ def test_append_step_with_a_bad_sentence_count(B, fmt, paged):
         else:
             for (x0, f0), (x1, f1) in zip(before[s], c.get(s, n)):
                 assert np.array_equal(x0, x1) and np.array_equal(f0, f1)
+
+
+# ------------------------------------------------------------------ tables of other slabs
+@pytest.mark.parametrize("paged", [False, True])
+def test_tables_of_more_sequences_are_taken(B, paged):
+    """A cache laid out for five sequences serves the first three of them; one of fewer, or with other heads, is refused."""
+    c = filled(B, [[100, 90]] * 5, [100] * 5, 2, "int8", 32, paged, 3, n_q=4)
+    q = queries(c, 4, 5)
+    whole = attend(c, q)
+    few = B.make_shape(3, 4, 2, 128, 1, 0, 1, c.max_cap, c.slab_off, c.cap, c.rows16)
+    out = torch.zeros(3, 4, 128, dtype=torch.bfloat16, device="cuda")
+    B.skipkv_decode_attn_q8(few, c.cache, q[:3], c.kv_len[:3], out, None, None, None, None, c.ws)
+    torch.cuda.synchronize()
+    assert c.status() == 0 and torch.equal(out, whole[:3])
+    for batch, heads in ((6, 2), (5, 1), (5, 4)):
+        shape = B.make_shape(batch, 2 * heads, heads, 128, 1, 0, 1, c.max_cap, c.slab_off, c.cap, c.rows16)
+        with pytest.raises(B.SkipKVError) as e:
+            B.skipkv_decode_attn_q8(shape, c.cache, q, c.kv_len, whole, None, None, None, None, c.ws)
+        assert e.value.code == -1

@@ -1,0 +1,37 @@
+"""Calls on the 8-bit cache and the page tables that would reach beyond their tables: refused before a launch, without a GPU."""
+import ctypes as C
+
+import pytest
+import torch
+
+
+@pytest.fixture(scope="module")
+def binding():
+    from paper_2512_07993_b200 import build, binding
+    build.build()
+    return binding
+
+
+@pytest.mark.parametrize("paged", [False, True])
+@pytest.mark.parametrize("batch,heads,code", [(1, 2, -1), (2, 1, -1), (2, 4, -1), (4, 1, -1), (0, 2, -1), (2, 0, -1)])
+def test_tables_of_other_slabs_are_refused(binding, paged, batch, heads, code):
+    """Scales or a block table for fewer sequences than the shape has, or for other KV heads.  (The pointers are never followed.)"""
+    lib = binding.lib()
+    shape = binding.make_shape(2, 8, 2, 128, 8, 256, 16, 256, None, None, 1024)
+    shape.slab_off, shape.cap = 256, 256
+    c = binding.Q8Cache(0, 64, 4, 2, -1, 0, 1024, 4096, 8192, 256, 512, 256 if paged else None, batch, heads)
+    s, k, p, q, none = C.byref(shape), C.byref(c), C.c_void_p(4096), C.c_void_p(8192), C.c_void_p(None)
+    assert lib.skipkv_pack_q8(s, k, p, p, p, p, none) == code
+    assert lib.skipkv_append_q8(s, k, p, p, p, 2, p, q, p, none) == code
+    assert lib.skipkv_append_step_q8(s, k, p, p, p, q, p, p, p, p, p, none, none, 0, p, none) == code
+    assert lib.skipkv_decode_attn_q8(s, k, p, p, p, none, none, none, none, p, none) == code
+    assert lib.skipkv_unpack_q8(s, k, p, p, p, p, none) == code
+
+
+def test_make_q8_cache_keeps_the_slabs_of_its_tables(binding, monkeypatch):
+    monkeypatch.setattr(binding, "_ptr", lambda t, dtype=None: None)
+    K = torch.zeros(256, 128, dtype=torch.int8)
+    c = binding.make_q8_cache(K, K, torch.zeros(3, 5, 2), torch.zeros(3, 5, 2), 64)
+    assert (c.batch, c.n_kv_heads) == (3, 5)
+    c = binding.make_q8_cache(K, K, torch.zeros(2, 2), torch.zeros(2, 2), 64, torch.zeros(4, 7, 1, dtype=torch.int32))
+    assert (c.batch, c.n_kv_heads) == (4, 7)
