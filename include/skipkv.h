@@ -538,7 +538,8 @@ int skipkv_unpack_q8(const skipkv_shape* shape, const skipkv_q8_cache* cache, co
  * come back in a call are handed out from the next call on.  The order is that of the slabs: the same tables from run to run.
  * need < 0, need beyond max_pages pages, n_pages_in outside [0, max_pages]: that slab is left as it is and SKIPKV_STATUS_BAD_TABLE is
  * raised; so it is where the ring is inconsistent (a page outside the pool, more pages than the pool has).  status: device uint32,
- * nullable, bits are OR-ed in.  At most 8192 slabs (SKIPKV_ERR_UNSUPPORTED).
+ * nullable, bits are OR-ed in.  At most 8192 slabs; block table entries and pool pages together, and the pool's rows, fewer than 2^31
+ * (SKIPKV_ERR_UNSUPPORTED).
  */
 int skipkv_page_tables(int32_t batch, int32_t n_kv_heads, int32_t max_pages, int32_t pool_pages, const int32_t* need,
                        const int32_t* n_pages_in, int32_t* n_pages_out, int32_t* block_table, int32_t* free_ring,

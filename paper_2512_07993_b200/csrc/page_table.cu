@@ -186,8 +186,8 @@ extern "C" int skipkv_page_tables(int32_t batch, int32_t n_kv_heads, int32_t max
         set_error_text("skipkv_page_tables: batch * n_kv_heads above 8192");
         return SKIPKV_ERR_UNSUPPORTED;
     }
-    // rows of the pool, places of the ring and sums over the slabs in 32 bits
-    if (int64_t(pool_pages) * SKIPKV_PAGE_ROWS > 0x7fffffff || slabs * max_pages > 0x7fffffff) return SKIPKV_ERR_UNSUPPORTED;
+    // rows of the pool, sums over the slabs, and places of the ring (free pages, then those that n_pages_in says are given back) in 32 bits
+    if (int64_t(pool_pages) * SKIPKV_PAGE_ROWS > 0x7fffffff || slabs * max_pages + pool_pages > 0x7fffffff) return SKIPKV_ERR_UNSUPPORTED;
     const size_t smem = size_t(3 * slabs + 2) * 4;
     const int64_t want = (slabs * 16 + kPtWarps - 1) / kPtWarps;       // 16 warps to a slab, as far as the SMs go
     const int grid = int(want < num_sms() ? want : num_sms());

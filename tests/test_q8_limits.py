@@ -35,3 +35,11 @@ def test_make_q8_cache_keeps_the_slabs_of_its_tables(binding, monkeypatch):
     assert (c.batch, c.n_kv_heads) == (3, 5)
     c = binding.make_q8_cache(K, K, torch.zeros(2, 2), torch.zeros(2, 2), 64, torch.zeros(4, 7, 1, dtype=torch.int32))
     assert (c.batch, c.n_kv_heads) == (4, 7)
+
+
+@pytest.mark.parametrize("slabs,max_pages,pool", [(1, (1 << 31) - 8, 16), (4, (1 << 29) - 1, 1 << 20), (8192, (1 << 18) - 1, 1 << 23)])
+def test_page_tables_whose_places_pass_32_bits_are_refused(binding, slabs, max_pages, pool):
+    """Counts that claim whole rows of the block table, given back behind the free pages: a place of the ring would be a sum beyond 2^31."""
+    assert slabs * max_pages < 1 << 31 <= slabs * max_pages + pool
+    p, q = C.c_void_p(4096), C.c_void_p(8192)
+    assert binding.lib().skipkv_page_tables(slabs, 1, max_pages, pool, p, p, q, p, p, p, q, None, None) == -2
