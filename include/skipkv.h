@@ -505,8 +505,10 @@ int skipkv_append_step_q8(const skipkv_shape* shape, const skipkv_q8_cache* cach
 
 /*
  * skipkv_decode_attn_q8 -- skipkv_decode_attn over an 8-bit cache: out[b][q] = sum_t softmax_t(q[b][q] . (s_k c_k)[t] / sqrt(d))
- * (s_v c_v)[t] for t < kv_len[b][q / n]; the codes take part as they are, sums and softmax are those of 32 bits (so logits and the sums of
- * p_t |s_v c_v|, p_t relative to the largest probability, have to stay below 2^127); bf16 result;
+ * (s_v c_v)[t] for t < kv_len[b][q / n]; bf16 result.  The codes take part as they are; logits, softmax and sums are those of 32 bits (so
+ * logits and the sums of p_t |s_v c_v|, p_t relative to the largest probability, have to stay below 2^127), with two roundings of factors:
+ * p_t goes into the products with the values in 22 bits, to 2^-40 where it is small; and an element of q below 2^-14 of its head's largest (INT8: 2^-31)
+ * is off by up to 2^-22 (2^-39) of that largest, which is nothing beside a product of the largest, but all there is where that one meets codes of 0.
  * kv_len == 0 gives zeros.  Lengths beyond a slab's room are taken as the room.  Everything else, the steering add included, as
  * skipkv_decode_attn.
  */

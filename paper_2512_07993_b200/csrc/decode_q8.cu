@@ -384,9 +384,10 @@ decode_q8_kernel(int batch, int Hq, int Hk, int n_slabs, const int64_t* slab_off
 
     // The B operand of S = K Q^T, times 2^shift; unshift takes the heads of the accumulator's columns back.
     //  int8 (codes as f16): step i has channels 32 qd + 4 i + {0, 1} in qa[2 i] and {2, 3} in qa[2 i + 1], the largest magnitude in
-    //  [2^14, 2^15); few heads: even columns only.
+    //  [2^14, 2^15), so the 8 bits are whole from 2^-17 on, 2^-31 of it, and smaller ones off by 2^-25; few heads: even columns only.
     //  e4m3 (codes as they are): the largest magnitude in [2^7, 2^8) and two e4m3 parts, high and 2^5 times the rest, together the 8 bits of
-    //  every bf16 from 2^-15 of the head's largest on (a smaller one is rounded to 2^-23 of that).  Step i has channels 32 qd + 8 i + {0 to 3} in
+    //  every bf16 from 2^-7 on, 2^-14 of the head's largest at most.  (A smaller one goes to the next multiple of 2^-14, the last place of the low part:
+    //  off by up to 2^-15, 2^-22 of the largest.  A third part would be a third product of every tile.)  Step i has channels 32 qd + 8 i + {0 to 3} in
     //  qa[2 i] and {4 to 7} in qa[2 i + 1]; low parts in odd columns (few heads) or in q_lo.
     float2 unshift = make_float2(1.f, 1.f);
     uint32_t q_lo[8];

@@ -1,5 +1,5 @@
 """The 8-bit cache at the ends of its ranges: infinities beside the largest magnitudes, sums and logits near the largest numbers, queries of very
-unequal elements, slabs that reach beyond their buffers, range lists that make no sense."""
+unequal elements, slabs that reach beyond their buffers, range lists that make no sense, tables of other slabs."""
 import numpy as np
 import pytest
 import torch
@@ -113,6 +113,39 @@ def test_attention_with_logits_far_below_zero(B, fmt, paged, group, n):
     q[:, :, 0] = 2.0 ** 60
     out = attend(c, q.bfloat16().cuda()).double().cpu().numpy()
     assert np.array_equal(out[0], np.broadcast_to(bf16(v[top]).double().numpy(), (group, 128)))
+
+
+# ------------------------------------------------------------------ queries of unequal elements
+@pytest.mark.parametrize("fmt,steps", [("e4m3", (9, 14, 16, 18, 30)), ("int8", (20, 31, 33, 35, 60))])
+@pytest.mark.parametrize("group", [3, 7])
+def test_attention_where_large_query_elements_meet_zeros(B, fmt, steps, group):
+    """One element is 2^step times the others and meets keys that are 0, so the others make the logits.  They are exact from 2^-14 (int8: 2^-31) of
+    the largest on; below that off by at most 2^-22 (2^-39) of it, which moves a logit by that times sum |k| / sqrt(d)."""
+    for step in steps:
+        c = filled(B, [[600, 77]], [600], 2, fmt, 16, False, 9, n_q=2 * group)
+        for s in range(2):
+            rows = torch.from_numpy(c.places(s, len(c.rows64[0][s]))[0]).cuda()
+            c.K[rows, 17] = 0
+            c.rows64[0][s][:, 17] = 0
+        q = queries(c, 2 * group, 7)
+        # others in [1, 2) in magnitude
+        q = (1 + q.float().abs().frac()).bfloat16().clamp(max=1.9921875) * torch.where(q < 0, -1, 1).bfloat16()
+        q[:, :, 17] = 2.0 ** step
+        out = attend(c, q)
+        if step <= (14 if fmt == "e4m3" else 31):
+            check_attention(c, q, out)
+            continue
+        lost = 2.0 ** step * (2.0 ** -22 if fmt == "e4m3" else 2.0 ** -39)
+        q64, got = q.double().cpu().numpy(), out.double().cpu().numpy()
+        for s in range(c.slabs):
+            K, V = c.rows64[0][s], c.rows64[1][s]
+            for j in range(group):
+                qq = q64[0, s * group + j][None]
+                want, mine = oracle.attn_rows(qq, K, V)[0], got[0, s * group + j]
+                e = (2.0 ** -23 * 136 * (np.abs(qq) @ np.abs(K).T).max() + lost * np.abs(K).sum(1).max()) / np.sqrt(128)
+                # a probability is off by a factor of at most exp(2 e)
+                room = 2.0 ** -8 * np.abs(want) + (1 + 2.0 ** -8) * ((np.expm1(min(2 * e, 50)) + 2.0 ** -19) * oracle.attn_rows(qq, K, np.abs(V))[0] + 2.0 ** -40 * np.abs(V).sum(0))
+                assert (np.abs(mine - want) <= room).all(), (step, s, j)
 
 
 # ------------------------------------------------------------------ slabs that reach beyond the buffers
