@@ -17,6 +17,7 @@ struct Q8View {
     float* v_scale;
     const int32_t* table;                     // nullptr: contiguous slabs
     long long rows;
+    int end;                                  // the same: fewer than 2^31
     int block_log2, max_blocks, max_pages;
 };
 
@@ -24,6 +25,7 @@ inline Q8View q8_view(const skipkv_q8_cache& c) {
     Q8View v{};
     v.K = static_cast<uint8_t*>(c.K); v.V = static_cast<uint8_t*>(c.V);
     v.k_scale = c.k_scale; v.v_scale = c.v_scale; v.table = c.block_table; v.rows = c.rows;
+    v.end = int(c.rows);
     v.block_log2 = c.block_rows == 16 ? 4 : c.block_rows == 32 ? 5 : c.block_rows == 64 ? 6 : 7;
     v.max_blocks = c.max_blocks; v.max_pages = c.max_pages;
     return v;
@@ -46,14 +48,11 @@ __host__ __device__ __forceinline__ int q8_row0(int64_t off, int cap, int Hk, in
 __host__ __device__ __forceinline__ int q8_row0(const int64_t* slab_off, const int32_t* cap, int Hk, int s) {
     return q8_row0(slab_off[s / Hk], cap[s / Hk], Hk, s);
 }
-// What of `room` rows from row0 on (as q8_row0 gives it) a buffer of `rows` rows has.
-__host__ __device__ __forceinline__ int rows_inside(int room, int row0, long long rows) {
-    return row0 < 0 ? 0 : int(max(0ll, min((long long)room, rows - row0)));
-}
-// Rows that slab s has room for, in the buffers too where it is contiguous.
+// Of `room` rows those that lie between row0 (as q8_row0 gives it) and the end of a buffer.
+__host__ __device__ __forceinline__ int rows_inside(int room, int row0, int end) { return row0 < 0 || row0 > end ? 0 : min(room, end - row0); }
+// Rows that a slab has room for, in the buffers too.
 __host__ __device__ __forceinline__ int q8_room_inside(const Q8View& v, int cap, int row0) {
-    const int room = q8_room(v, cap);
-    return v.table ? room : rows_inside(room, row0, v.rows);
+    return v.table ? q8_room(v, cap) : rows_inside(q8_room(v, cap), row0, v.end);
 }
 // Where tile j (tokens [128 j, 128 j + 128)) of slab s lies: its first row, and the place of its first block's scale.  Of its first
 // `rows` rows none may lie outside the buffers, else row = -1.  row0: as q8_row0 gives it (not used for a paged cache).
