@@ -445,7 +445,7 @@ int skipkv_decode_attn_static(const skipkv_shape* shape, const void* q, const vo
  * not in [0, rows / SKIPKV_PAGE_ROWS), a slab that reaches beyond `rows`) are neither read nor written: SKIPKV_STATUS_BAD_TABLE is
  * raised, and attention and skipkv_unpack_q8 go on with the others.  Two slabs must not share a page that a call writes (reading a shared one is fine).  None of
  * these calls waits for anything on the GPU but the work before it on the stream: the wait limit does not concern them.  At most 8192
- * slabs, and fewer than 2^30 scales in a table of contiguous slabs or entries in a block table (SKIPKV_ERR_UNSUPPORTED).
+ * slabs, and fewer than 2^30 - 4096 scales in a table of contiguous slabs or entries in a block table (SKIPKV_ERR_UNSUPPORTED).
  */
 #define SKIPKV_Q8_E4M3 0
 #define SKIPKV_Q8_INT8 1

@@ -560,8 +560,8 @@ int check_q8(const skipkv_shape* s, const skipkv_q8_cache* c) {
         set_error_text("8-bit cache: batch * n_kv_heads above 8192");
         return SKIPKV_ERR_UNSUPPORTED;
     }
-    // places of scales, and tiles of K and V of all slabs, in 32 bits
-    if (slabs * (c->block_table ? c->max_pages : c->max_blocks) >= 1 << 30) return SKIPKV_ERR_UNSUPPORTED;
+    // places of scales, and tiles of K and V of all slabs with a grid's step more, in 32 bits
+    if (slabs * (c->block_table ? c->max_pages : c->max_blocks) >= (1 << 30) - 4096) return SKIPKV_ERR_UNSUPPORTED;
     if (c->device >= 0) {
         int dev = 0;
         SKIPKV_CUDA(cudaGetDevice(&dev));

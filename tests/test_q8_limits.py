@@ -43,3 +43,19 @@ def test_page_tables_whose_places_pass_32_bits_are_refused(binding, slabs, max_p
     assert slabs * max_pages < 1 << 31 <= slabs * max_pages + pool
     p, q = C.c_void_p(4096), C.c_void_p(8192)
     assert binding.lib().skipkv_page_tables(slabs, 1, max_pages, pool, p, p, q, p, p, p, q, None, None) == -2
+
+
+@pytest.mark.parametrize("over", [dict(max_blocks=(1 << 28) - 2), dict(block_table=256, max_pages=(1 << 28) - 2)])
+def test_tables_whose_last_step_passes_32_bits_are_refused(binding, over):
+    """Four slabs with all but eight of 2^30 places: a CTA's step behind the last tile of K and V would be a number beyond 2^31."""
+    lib = binding.lib()
+    shape = binding.make_shape(2, 8, 2, 128, 8, 256, 16, 256, None, None, 1024)
+    shape.slab_off, shape.cap = 256, 256
+    c = binding.Q8Cache(0, 64, 4, 2, -1, 0, 1024, 4096, 8192, 256, 512, None)
+    for k, v in over.items():
+        setattr(c, k, v)
+    s, k, p, q, none = C.byref(shape), C.byref(c), C.c_void_p(4096), C.c_void_p(8192), C.c_void_p(None)
+    assert lib.skipkv_unpack_q8(s, k, p, p, p, p, none) == -2
+    assert lib.skipkv_pack_q8(s, k, p, p, p, p, none) == -2
+    assert lib.skipkv_append_q8(s, k, p, p, p, 2, p, q, p, none) == -2
+    assert lib.skipkv_decode_attn_q8(s, k, p, p, p, none, none, none, none, p, none) == -2
