@@ -34,10 +34,10 @@ int check_q8(const skipkv_shape* s, const skipkv_q8_cache* c);      // SKIPKV_OK
 
 #ifdef __CUDACC__
 
-// Rows that a slab of `cap` rows has room for.
+// Rows that a slab of `cap` rows has room for: in any case so few that a tile's rows more are a number of 32 bits.
 __host__ __device__ __forceinline__ int q8_room(const Q8View& v, int cap) {
     const long long lim = v.table ? (long long)v.max_pages * kQ8Tile : (long long)v.max_blocks << v.block_log2;
-    return int(min((long long)max(cap, 0), lim));
+    return min(max(cap, 0), int(min(lim, 0x7fffff00ll)));
 }
 __host__ __device__ __forceinline__ int q8_room(const Q8View& v, const int32_t* cap, int Hk, int s) { return q8_room(v, cap[s / Hk]); }
 __host__ __device__ __forceinline__ int q8_row0(int64_t off, int cap, int Hk, int s) {

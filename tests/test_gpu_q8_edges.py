@@ -286,9 +286,11 @@ def test_tables_of_more_sequences_are_taken(B, paged):
     whole = attend(c, q)
     few = B.make_shape(3, 4, 2, 128, 1, 0, 1, c.max_cap, c.slab_off, c.cap, c.rows16)
     out = torch.zeros(3, 4, 128, dtype=torch.bfloat16, device="cuda")
-    B.skipkv_decode_attn_q8(few, c.cache, q[:3], c.kv_len[:3], out, None, None, None, None, c.ws)
+    ws = torch.empty(B.skipkv_workspace_bytes(few), dtype=torch.uint8, device="cuda")
+    B.skipkv_workspace_init(few, ws)
+    B.skipkv_decode_attn_q8(few, c.cache, q[:3], c.kv_len[:3], out, None, None, None, None, ws)
     torch.cuda.synchronize()
-    assert c.status() == 0 and torch.equal(out, whole[:3])
+    assert B.skipkv_status(ws) == 0 and torch.equal(out, whole[:3])
     for batch, heads in ((6, 2), (5, 1), (5, 4)):
         shape = B.make_shape(batch, 2 * heads, heads, 128, 1, 0, 1, c.max_cap, c.slab_off, c.cap, c.rows16)
         with pytest.raises(B.SkipKVError) as e:

@@ -1,8 +1,12 @@
 """Calls on the 8-bit cache and the page tables that would reach beyond their tables: refused before a launch, without a GPU."""
 import ctypes as C
+import os
+import subprocess
 
 import pytest
 import torch
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
 
 @pytest.fixture(scope="module")
@@ -59,3 +63,40 @@ def test_tables_whose_last_step_passes_32_bits_are_refused(binding, over):
     assert lib.skipkv_pack_q8(s, k, p, p, p, p, none) == -2
     assert lib.skipkv_append_q8(s, k, p, p, p, 2, p, q, p, none) == -2
     assert lib.skipkv_decode_attn_q8(s, k, p, p, p, none, none, none, none, p, none) == -2
+
+
+# ------------------------------------------------------------------ the kernels' counts, compiled for the host
+COUNTS = r"""
+#include <climits>
+#include <cstdio>
+#include "q8.cuh"
+using namespace skipkv;
+int main() {
+    const int caps[] = {INT_MIN, -1, 0, 1, 128, 0x7ffffeff, 0x7fffff00, 0x7fffff01, INT_MAX - 1, INT_MAX};
+    for (int paged = 0; paged < 2; ++paged)
+        for (int log2 = 4; log2 <= 7; ++log2)
+            for (int most : {1, 1 << 20, 1 << 24, 1 << 25, (1 << 30) - 5000})
+                for (int cap : caps) {
+                    Q8View v{};
+                    int32_t table = 0;
+                    v.table = paged ? &table : nullptr;
+                    v.block_log2 = log2; v.max_blocks = v.max_pages = most;
+                    const int room = q8_room(v, cap);
+                    // the tiles of a slab that is full, as the kernels count them
+                    const unsigned tiles = unsigned(room) + unsigned(kQ8Tile) - 1u;
+                    if (room < 0 || room > (cap < 0 ? 0 : cap) || tiles > unsigned(INT_MAX)) { printf("%d %d %d %d: %d\n", paged, log2, most, cap, room); return 1; }
+                }
+    return 0;
+}
+"""
+
+
+def test_tiles_of_the_longest_slab_are_numbers_of_32_bits(binding, tmp_path):
+    """Whatever a table of capacities says: 127 rows more than a slab's room, the sum from which its tiles are counted, stay below 2^31."""
+    from paper_2512_07993_b200 import build
+    src, exe = tmp_path / "counts.cu", tmp_path / "counts"
+    src.write_text(COUNTS)
+    subprocess.run([build.NVCC, "-std=c++17", "-gencode", "arch=compute_100a,code=sm_100a", "-I", os.path.join(ROOT, "include"), "-I", build.CSRC,
+                    str(src), "-o", str(exe)], check=True)
+    got = subprocess.run([str(exe)], capture_output=True, text=True)
+    assert got.returncode == 0, got.stdout
