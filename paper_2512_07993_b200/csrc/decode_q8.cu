@@ -20,9 +20,10 @@
 //    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates), times the scale and 2^-15: sums of p |v| may reach 2^127.  Up to four heads per group the eight columns hold the
 //    high and low parts of a head side by side, so that a lane has one head to exponentiate.
 //  * An arrival's answer is not waited for before the CTA's next part; the last CTA of a slab loads its partials 16 at a time.
-// What it takes (back to back, and what bounds it): one sequence of 2048 tokens 7.4 us, latency (wait 0.9, first rows 2.0, a tile 0.9, its warps
-// merged 0.6, arrival 0.9, merge 1.3); 80 slabs of 4.1K 19.4 us, 0.66 of the copy rate: head and tail of a launch, between them 7.5 TB/s into the SMs; 128 slabs of 8.2K
-// behind pages, int8, five heads 50.2 us, 0.81: conversions and latency; 128 slabs of 32K to 64K 240 us, 1.02, and 280 in seconds of it (power).
+// What it takes (back to back, some hundred calls, and what bounds it): one sequence of 2048 tokens 7.4 us, latency (wait 0.9, first rows 2.0, a tile 0.9, its warps
+// merged 0.6, arrival 0.9, merge 1.3); 80 slabs of 4.1K 19.4 us, 0.66 of the copy rate: head and tail of a launch, between them 6.8 to 7.5 TB/s into the SMs; 128 slabs of
+// 8.2K behind pages, int8, five heads 49.8 us, 0.82: conversions and latency; 128 slabs of 32K to 64K 241 to 250 us, 0.98 to 1.02.  In seconds of it the power limit
+// takes the clock down: 55 and 285 us for the last two.
 #include <type_traits>
 
 #include "common.cuh"

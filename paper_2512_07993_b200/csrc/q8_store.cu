@@ -307,8 +307,8 @@ q8_store_kernel(int n_slabs, StoreSlabs<kAppend> slabs, StoreArgs a, const int* 
 // lengths and offsets are requested together, the rows and the scale behind them (paged: behind the page's entry); the codes that a block has are
 // touched only where its scale grows.  A call takes it with up to four rows per sequence: the general kernel enumerates tiles first and has one step
 // of the work (a tile) go through each CTA after the other.  Eight heads, us here / there: 16 sequences with a row each 2.0 / 5.7, four each 2.2 / 5.7;
-// 256 sequences 3.4 / 33 and 6.6 / 33.  Where one sequence has all the rows (of 16 to 64, or 256 sequences) it is 3.0 / 4.5, 7.2 / 4.6 and, with
-// 1024 rows, 28 / 8: the offsets are on the GPU, and that is the rarer case.  Four parts cost more than they give where there is a row to a
+// 256 sequences 3.0 / 33 and 6.6 / 33.  Where one sequence has all the rows (of 16 to 64, or 256 sequences) it is 3.0 / 4.5, 7.2 / 4.6 and, with
+// 1024 rows, 31 / 8: the offsets are on the GPU, and that is the rarer case.  Four parts cost more than they give where there is a row to a
 // sequence: 256 sequences 6.3 against 3.4.
 constexpr int kQoThreads = 128;
 constexpr int kQoMost = 4;                                     // rows per sequence, on average
