@@ -443,8 +443,8 @@ int skipkv_decode_attn_static(const skipkv_shape* shape, const void* q, const vo
  * code of its sign, a NaN as 0, and SKIPKV_STATUS_NOT_FINITE is raised.  Codes and scales are the same bits from run to run.
  * The reading calls and an append to a block take any scales from 2^-111 to 2^122.  Rows that lie outside the buffers (a page that is
  * not in [0, rows / SKIPKV_PAGE_ROWS), a slab that reaches beyond `rows`) are neither read nor written: SKIPKV_STATUS_BAD_TABLE is
- * raised, and attention and skipkv_unpack_q8 go on with the others.  Two slabs must not share a page that a call writes (reading a shared one is fine).  None of
- * these calls waits for anything on the GPU but the work before it on the stream: the wait limit does not concern them.  At most 8192
+ * raised, and attention and skipkv_unpack_q8 go on with the others.  Two slabs must not share a page that a call writes (reading
+ * a shared one is fine).  None of these calls waits for anything on the GPU but the work before it on the stream: the wait limit does not concern them.  At most 8192
  * slabs, and fewer than 2^30 - 4096 scales in a table of contiguous slabs or entries in a block table (SKIPKV_ERR_UNSUPPORTED).
  */
 #define SKIPKV_Q8_E4M3 0
@@ -507,8 +507,9 @@ int skipkv_append_step_q8(const skipkv_shape* shape, const skipkv_q8_cache* cach
  * skipkv_decode_attn_q8 -- skipkv_decode_attn over an 8-bit cache: out[b][q] = sum_t softmax_t(q[b][q] . (s_k c_k)[t] / sqrt(d))
  * (s_v c_v)[t] for t < kv_len[b][q / n]; bf16 result.  The codes take part as they are; logits, softmax and sums are those of 32 bits (so
  * logits and the sums of p_t |s_v c_v|, p_t relative to the largest probability, have to stay below 2^127), with two roundings of factors:
- * p_t goes into the products with the values in 22 bits, to 2^-40 where it is small; and an element of q below 2^-14 of its head's largest (INT8: 2^-31)
- * is off by up to 2^-22 (2^-39) of that largest, which is nothing beside a product of the largest, but all there is where that one meets codes of 0.
+ * p_t goes into the products with the values in 22 bits, to 2^-40 where it is small; and an element of q below 2^-14 of its head's largest
+ * (INT8: 2^-31) is off by up to 2^-22 (2^-39) of that largest, which is nothing beside a product of the largest, but counts where that one
+ * meets codes of 0.
  * kv_len == 0 gives zeros.  Lengths beyond a slab's room are taken as the room.  Everything else, the steering add included, as
  * skipkv_decode_attn.
  */

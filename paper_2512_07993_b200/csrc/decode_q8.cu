@@ -17,8 +17,8 @@
 //    which byte permutes make pairs of tokens.  Rows are 128 bytes; their 16-byte pieces lie permuted (piece c of row r at c ^ (r & 7)), so
 //    neither load has bank conflicts.
 //  * The probabilities go in as two f16 parts of 2^15 p, 22 bits of the fp32 value, absolute 2^-40 for small ones; a tile's products are added to the
-//    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates), times the scale and 2^-15: sums of p |v| may reach 2^127.  Up to four heads per group the eight columns hold the
-//    high and low parts of a head side by side, so that a lane has one head to exponentiate.
+//    sums over the tiles in fp32 with rounding (the tensor core's own accumulation truncates), times the scale and 2^-15: sums of
+//    p |v| may reach 2^127.  Up to four heads per group the eight columns hold the high and low parts of a head side by side, so that a lane has one head to exponentiate.
 //  * An arrival's answer is not waited for before the CTA's next part; the last CTA of a slab loads its partials 16 at a time.
 // What it takes (back to back, some hundred calls, and what bounds it): one sequence of 2048 tokens 7.4 us, latency (wait 0.9, first rows 2.0, a tile 0.9, its warps
 // merged 0.6, arrival 0.9, merge 1.3); 80 slabs of 4.1K 19.4 us, 0.66 of the copy rate: head and tail of a launch, between them 6.8 to 7.5 TB/s into the SMs; 128 slabs of
